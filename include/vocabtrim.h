@@ -54,7 +54,8 @@ enum {
     VT_FLAG_BAD_MAP = 2u,  /* vt_trim_head saw map entries outside [0,V); those rows were zero-filled */
     VT_FLAG_BAD_TEMP = 4u, /* vt_draft_head saw T <= 0, NaN or Inf; that row reports id -1, logprob NaN */
     VT_FLAG_NAN_ROW = 8u,  /* vt_draft_head produced no finite candidate for a row (NaN inputs)        */
-    VT_FLAG_TIMEOUT = 16u  /* a bounded device-side wait expired                                      */
+    VT_FLAG_TIMEOUT = 16u, /* a bounded device-side wait expired                                      */
+    VT_FLAG_BAD_PAGE = 32u /* a vt_kv_* call met a sequence, place, page, node or count out of range; it was left out */
 };
 
 /* Operation selectors for vt_workspace_bytes. */
@@ -65,7 +66,8 @@ enum {
     VT_OP_TRIM_HEAD = 3,
     VT_OP_DRAFT_HEAD = 4,
     VT_OP_DRAFT_HEAD_HOST = 5,
-    VT_OP_BUILD_VOCAB_HOST = 6
+    VT_OP_BUILD_VOCAB_HOST = 6,
+    VT_OP_KV_ATTEND = 7    /* n: sequences, B: new rows of each, K: query heads, V: key heads, d: head size */
 };
 
 #define VT_MAX_TOPK 64
@@ -323,6 +325,109 @@ vt_status vt_draft_head_host(const uint16_t *h_host, const uint16_t *W_trim, con
                              int32_t B, int32_t K, int32_t d, const float *temp_host,
                              int32_t topk, const float *uniforms_host, int32_t *out_ids_host,
                              float *out_logprobs_host, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * ---- The drafter's key-value cache ------------------------------------------------------------------
+ * Algorithm 2's drafter forward runs the drafter's body in front of the head; what it keeps from step to
+ * step is a key and a value of every token, in pages.  The four calls here write it, attend over it, move
+ * an accepted path into place and read it back.  (The paper leaves the body to its models and gives no
+ * formulas for it; head layouts are those of its drafters.)
+ *
+ * A sequence's token i lies in page pages[s][i / page], place i % page.  Places [0, lens[s]) hold the
+ * committed tokens; while a tree is drafted, its node f lies at place lens[s] + f.
+ *
+ *   k, v          DEVICE [n_pages, heads, page, d] by the three strides (in elements, positive; dims of a
+ *                 row adjacent), bf16 or e4m3; rows start at multiples of 16 bytes.  d: 64, 96, 128, 192 or 256.
+ *   k_exp, v_exp  VT_KV_E4M3: DEVICE uint8 [n_pages, heads, page], contiguous, 16-byte aligned.  A row stands
+ *                 for its e4m3 values times 2^(exp - 127), the smallest power that brings its largest
+ *                 magnitude to at most 448 (2^-126 at the least).  255: the row held a NaN or an infinity and
+ *                 reads as NaN.  The bytes 0x7f and 0xff are not written.  VT_KV_BF16: NULL.
+ *   pages         DEVICE int32 [S, max_pages], rows pages_ld >= max_pages apart; max_pages * page < 2^31.
+ *
+ * Sequences, places, pages and nodes out of range are left out (not written, not seen, read as zeros) and
+ * raise VT_FLAG_BAD_PAGE in the workspace, where one is given.  Two rows of a call for the same place, or a page
+ * that two sequences write, leave either row's bytes.
+ */
+#define VT_KV_BF16 0
+#define VT_KV_E4M3 1
+#define VT_KV_MAX_NEW 64     /* new rows of a sequence in one vt_kv_attend */
+#define VT_KV_MAX_NODES 2048 /* nodes of a sequence's tree in vt_kv_attend */
+typedef struct {
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;
+    int32_t format, n_pages, heads, page, d;
+    int64_t stride_page, stride_head, stride_token;
+    const int32_t *pages;
+    int32_t S, max_pages;
+    int64_t pages_ld;
+} vt_kv_cache;
+
+/*
+ * Frequencies of a rotation of `rot` dims: freqs[i] (HOST int64 [rot/2]) = base^(-2i/rot) / (2 pi), the turns a
+ * position makes, in units of 2^-64 (as unsigned).  factor > 1 stretches them the way Llama 3 does:
+ * wavelengths above original / low_factor by `factor`, those below original / high_factor not, in between
+ * in proportion.  HOST arithmetic.  rot % 16 == 0, 16 <= rot <= 256, base > 1, factor >= 1,
+ * 0 < low_factor < high_factor, original > 0 (the last three are not looked at when factor == 1).
+ */
+vt_status vt_rope_freqs(int32_t rot, double base, double factor, double low_factor, double high_factor,
+                        double original, int64_t *freqs);
+
+/*
+ * T new tokens: norms of queries and keys, rotation, and the write into the cache, in one pass.
+ *   q [T,Hq,d], k, v [T,heads,d] bf16, 16-byte aligned, tokens q_ld, k_ld, v_ld elements apart (multiples of 8, at least
+ *   a token's heads), heads side by side: the parts of one projection's output fit.  q NULL (Hq = 0): keys and values only.
+ *   q_weight, k_weight [d] bf16 or NULL: x * rsqrt(mean(x^2) + eps) * weight per head
+ *   freqs [rot/2] (DEVICE, of vt_rope_freqs) and positions [T], or NULL, rot = 0: pairs (i, i + rot/2), or (2i, 2i+1)
+ *     with interleaved != 0, of the first rot dims are rotated by positions[t]; far positions lose nothing (the angle is
+ *     taken modulo one turn in whole numbers)
+ *   seq [T] or NULL: the token's sequence (NULL: T / S rows of each in order, T % S == 0)
+ *   index [T]: its place in the sequence; negative: not written (q is made all the same)
+ *   q_out [T,Hq,d] bf16 (may be q where that is contiguous)
+ * Arithmetic in fp32 and one rounding to bf16; keys of an e4m3 cache in fp64, so that every stored byte is the
+ * correctly rounded one.  `ws`: NULL, or a workspace for the flag.  T = 0: no-op.
+ */
+vt_status vt_qkv_write(const uint16_t *q, int64_t q_ld, const uint16_t *k, int64_t k_ld, const uint16_t *v, int64_t v_ld,
+                       int32_t T, int32_t Hq, const vt_kv_cache *cache, const int32_t *seq, const int32_t *index,
+                       const int32_t *positions, const int64_t *freqs, int32_t rot, int32_t interleaved,
+                       const uint16_t *q_weight, const uint16_t *k_weight, double eps, uint16_t *q_out, void *ws,
+                       void *stream);
+
+/*
+ * Reads T rows back: k_out, v_out [T,heads,d] bf16 = the rows at places index[t] of sequences seq[t] (NULL as above);
+ * negative or out of range: zeros.  Exact for both formats, but for e4m3 values beyond bf16's range.
+ */
+vt_status vt_kv_read(const vt_kv_cache *cache, const int32_t *seq, const int32_t *index, int32_t T, uint16_t *k_out,
+                     uint16_t *v_out, void *ws, void *stream);
+
+/*
+ * Attention of Q new rows of each of S sequences (rows s * Q .. of q and out):
+ *   out = sum_t p_t v_t / sum_t p_t, p_t = exp(scale * q . k_t), lse = log sum_t p_t, over the places t < lens[s] and, with
+ *   `node`, those of the row's node and its ancestors.
+ *   q [S*Q,Hq,d] bf16, rows q_ld elements apart (a multiple of 8, at least Hq * d); Hq a multiple of the cache's heads, query head h
+ *     reads key head h / (Hq / heads); Q <= VT_KV_MAX_NEW
+ *   lens [S]: the committed tokens (below 0: 0; more than the page table holds: what it holds)
+ *   node [S*Q] or NULL (rows see the committed tokens alone): the row's node, -1 = the committed prefix alone, below -1 = no token
+ *     at all (a row of padding); N or more: flagged, the prefix alone
+ *   parent [S,N], rows parent_ld apart, or NULL: node i's parent, -1 = child of the prefix; what is not in [-1, i) ends the walk.
+ *     NULL: chains (parent[i] = i - 1).  N <= VT_KV_MAX_NODES; N is looked at with `node` only.
+ *   out [S*Q,Hq,d] bf16; lse [S*Q,Hq] fp32 or NULL.  A row whose weights sum to zero (it sees no token, or scores of -inf) has
+ *     zeros and an lse of -inf.
+ * Sums, maxima and scores are fp32, weights enter the products as two bf16 pieces.  Sequences may have any lengths;
+ * results are the same from call to call.  Workspace: vt_workspace_bytes(VT_OP_KV_ATTEND, ...).
+ */
+vt_status vt_kv_attend(const uint16_t *q, int64_t q_ld, int32_t Q, int32_t Hq, const vt_kv_cache *cache, const int32_t *lens,
+                       const int32_t *node, const int32_t *parent, int64_t parent_ld, int32_t N, float scale,
+                       uint16_t *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The accepted nodes of vt_verify_greedy become committed tokens: for i < n_accept[s] the row of node path[s][i], or of
+ * nodes[s][path[s][i]] where `nodes` is given (vt_tree_rerank's out_nodes: the draft's positions as nodes of the pool), moves to
+ * place lens[s] + i.  path, nodes [S,N]; a node smaller than i is out of range (paths rise).
+ * new_lens [S] or NULL receives lens[s] + n_accept[s]; it may be `lens`.  A bit copy; every layer's cache is moved by
+ * a call of its own, with the old lens.  lens or n_accept out of range: nothing moves.  `ws` as above.
+ */
+vt_status vt_kv_commit(const vt_kv_cache *cache, const int32_t *lens, const int32_t *path, const int32_t *n_accept,
+                       const int32_t *nodes, int32_t N, int32_t *new_lens, void *ws, void *stream);
 
 #ifdef VT_STAMPS
 /*

@@ -23,7 +23,10 @@ LIB_PATH = os.path.join(_HERE, "libvocabtrim.so")
 VT_OK = 0
 VT_OP_HISTOGRAM, VT_OP_SELECT_TOPK, VT_OP_BUILD_VOCAB, VT_OP_TRIM_HEAD = 0, 1, 2, 3
 VT_OP_DRAFT_HEAD, VT_OP_DRAFT_HEAD_HOST, VT_OP_BUILD_VOCAB_HOST = 4, 5, 6
+VT_OP_KV_ATTEND = 7                                  # workspace_bytes: n sequences, B new rows of each, K query heads, V key heads, d
 VT_FLAG_BAD_ID, VT_FLAG_BAD_MAP, VT_FLAG_BAD_TEMP, VT_FLAG_NAN_ROW, VT_FLAG_TIMEOUT = 1, 2, 4, 8, 16
+VT_FLAG_BAD_PAGE = 32
+VT_KV_MAX_NEW, VT_KV_MAX_NODES = 64, 2048
 VT_MAX_TOPK = 64
 VT_CTRL_BYTES = 256
 
@@ -33,6 +36,7 @@ EXPORTS = (
     "vt_histogram", "vt_histogram_folded", "vt_select_topk", "vt_build_vocab", "vt_build_vocab_host", "vt_trim_head",
     "vt_draft_head", "vt_draft_head_debug", "vt_draft_head_host", "vt_select_topk_static",
     "vt_draft_head_overlapped", "vt_select_topp", "vt_select_minfreq", "vt_verify_greedy", "vt_mbsu", "vt_tree_expand", "vt_tree_rerank", "vt_draft_head_expand",
+    "vt_rope_freqs", "vt_qkv_write", "vt_kv_read", "vt_kv_attend", "vt_kv_commit",
 )
 
 
@@ -46,7 +50,7 @@ class VocabTrimError(RuntimeError):
 _lib = None
 _bind = None                                       # the calls a program makes per step or per build, marshalled in C++ (csrc/vt_bind.cpp)
 _BOUND = ("vt_draft_head", "vt_draft_head_overlapped", "vt_draft_head_host", "vt_draft_head_expand", "vt_tree_rerank", "vt_verify_greedy",
-          "vt_build_vocab", "vt_trim_head")
+          "vt_build_vocab", "vt_trim_head", "vt_qkv_write", "vt_kv_read", "vt_kv_attend", "vt_kv_commit")
 
 
 def lib() -> ctypes.CDLL:
@@ -88,6 +92,13 @@ def lib() -> ctypes.CDLL:
         L.vt_draft_head_overlapped.argtypes = head
         L.vt_draft_head_host.argtypes = head
         L.vt_draft_head_debug.argtypes = head + [c_void_p, c_void_p]
+        L.vt_rope_freqs.argtypes = [c_int32] + [c_double] * 5 + [c_void_p]
+        L.vt_qkv_write.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_double, c_void_p, c_void_p, c_void_p]
+        L.vt_kv_read.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.vt_kv_attend.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_float, c_void_p,
+                                   c_void_p, c_void_p, c_size_t, c_void_p]
+        L.vt_kv_commit.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p]
         try:
             from . import _vt_bind as bind
         except ImportError as e:
@@ -396,3 +407,77 @@ def vt_draft_head_host(h_host: torch.Tensor, W_trim: torch.Tensor, map_: torch.T
     _lib or lib()
     _check("vt_draft_head_host", _bind.draft_head_host(h_host, W_trim, map_, B, K, d, temp_host, topk, uniforms_host, ids, lps, ws))
     return ids, lps
+
+
+def kv_cache(n_pages: int, heads: int, page: int, d: int, e4m3: bool = False, device="cuda"):
+    """Caller-owned paged cache of the vt_kv_* calls: (k, v, k_exp, v_exp), k and v [n_pages, heads, page, d] in bf16, or in e4m3 with
+    the exponents of their rows, uint8 [n_pages, heads, page].  Any other tensors of these shapes do as well: the first three strides of k and
+    v are free, as long as rows start at multiples of 16 bytes."""
+    kw = {"dtype": torch.float8_e4m3fn if e4m3 else torch.bfloat16, "device": device}
+    k, v = (torch.empty((n_pages, heads, page, d), **kw) for _ in range(2))
+    exps = tuple(torch.empty((n_pages, heads, page), dtype=torch.uint8, device=device) for _ in range(2)) if e4m3 else (None, None)
+    return (k, v) + exps
+
+
+def vt_rope_freqs(rot: int, base: float = 10000.0, factor: float = 1.0, low_factor: float = 1.0, high_factor: float = 4.0,
+                  original: float = 8192.0, device="cuda") -> torch.Tensor:
+    """Frequencies of a rotation of `rot` dims for vt_qkv_write, int64 [rot/2] (turns a position, in units of 2^-64).  factor > 1
+    stretches them the way Llama 3 does."""
+    freqs = torch.empty(max(rot, 0) // 2, dtype=torch.int64)
+    _check("vt_rope_freqs", lib().vt_rope_freqs(rot, base, factor, low_factor, high_factor, original, freqs.data_ptr()))
+    return freqs.to(device)
+
+
+def vt_qkv_write(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, cache, pages: torch.Tensor, index: torch.Tensor,
+                 seq: torch.Tensor | None = None, positions: torch.Tensor | None = None, freqs: torch.Tensor | None = None,
+                 q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+                 interleaved: bool = False, out: torch.Tensor | None = None, ws: Workspace | None = None):
+    """New tokens in front of the drafter's attention (Algorithm 2, drafter forward): norms of queries and keys per head (where a weight is
+    given), rotation (where freqs are given), and keys and values into the paged cache at place index[t] of sequence seq[t], in one pass.
+
+    q [T,Hq,d] or None, k and v [T,heads,d] bf16 (parts of one projection's output fit); pages int32 [S,max_pages];
+    index, seq, positions int32 [T]; seq None: T/S rows of each sequence in order; a negative index is not written.  Returns the
+    queries as bf16 [T,Hq,d] (None without q).  ws: where VT_FLAG_BAD_PAGE goes."""
+    _lib or lib()
+    r = _bind.qkv_write(q, k, v, cache, pages, index, seq, positions, freqs, q_weight, k_weight, eps, interleaved, out, ws)
+    if r.__class__ is int:
+        raise VocabTrimError("vt_qkv_write", r)
+    return r
+
+
+def vt_kv_read(cache, pages: torch.Tensor, index: torch.Tensor, seq: torch.Tensor | None = None, out=None, ws: Workspace | None = None):
+    """Cached rows as bf16: (k, v), each [T,heads,d], of places index[t] of sequences seq[t] (as vt_qkv_write takes them); negative or out of
+    range: zeros."""
+    _lib or lib()
+    r = _bind.kv_read(cache, pages, index, seq, out, ws)
+    if r.__class__ is int:
+        raise VocabTrimError("vt_kv_read", r)
+    return r
+
+
+def vt_kv_attend(q: torch.Tensor, cache, pages: torch.Tensor, lens: torch.Tensor, node: torch.Tensor | None = None,
+                 parent: torch.Tensor | None = None, scale: float | None = None, out=None, ws: Workspace | None = None):
+    """Attention of Q new rows of each of S sequences over the paged cache (Algorithm 2, drafter forward): a row sees the lens[s]
+    committed tokens and, with `node`, its node of the draft tree and the node's ancestors, which lie at places lens[s] + node.
+
+    q bf16 [S*Q,Hq,d]; lens int32 [S]; node int32 [S*Q] (-1: the committed tokens alone, below: no token); parent int32 [S,N] (None:
+    chains).  For a drafting loop node is the frontier and parent[s] the pool's.  scale None: 1/sqrt(d).  Returns (out bf16
+    [S*Q,Hq,d], lse fp32 [S*Q,Hq]); a row that sees nothing has zeros and -inf."""
+    _lib or lib()
+    r = _bind.kv_attend(q, cache, pages, lens, node, parent, scale, out, ws)
+    if r.__class__ is int:
+        S = pages.shape[0]
+        _fail("vt_kv_attend", r, VT_OP_KV_ATTEND, (S, cache[0].shape[1], q.shape[1], q.shape[2], q.shape[0] // S if S else 1), ws)
+    return r
+
+
+def vt_kv_commit(cache, pages: torch.Tensor, lens: torch.Tensor, path: torch.Tensor, n_accept: torch.Tensor,
+                 nodes: torch.Tensor | None = None, out: torch.Tensor | None = None, ws: Workspace | None = None) -> torch.Tensor:
+    """Accepted nodes become committed tokens (Algorithm 2's accept loop): the cached row of path[s][i], i < n_accept[s], moves to place
+    lens[s] + i.  path and n_accept as vt_verify_greedy returns them; nodes int32 [S,N]: the draft's nodes in the pool (vt_tree_rerank's
+    first output) where the cache was written by pool node.  Returns the new lengths [S]; out may be lens."""
+    _lib or lib()
+    r = _bind.kv_commit(cache, pages, lens, path, n_accept, nodes, out, ws)
+    if r.__class__ is int:
+        raise VocabTrimError("vt_kv_commit", r)
+    return r

@@ -3,6 +3,7 @@
 #include <atomic>
 
 #include "vt_common.cuh"
+#include "vt_kv.cuh"
 
 #include <cmath>
 #include <cstdint>
@@ -72,6 +73,36 @@ HostStage host_stage(int32_t B, int32_t K, int32_t d, int32_t topk, size_t base)
     return s;
 }
 
+bool kv_head_size_ok(int32_t d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
+
+bool kv_attend_shape_ok(int64_t S, int32_t Q, int32_t Hq, int32_t heads, int32_t d) {
+    return S >= 0 && S <= INT32_MAX && Q >= 1 && Q <= VT_KV_MAX_NEW && heads >= 1 && Hq >= heads && Hq % heads == 0 && Hq <= 1024 && kv_head_size_ok(d);
+}
+
+// A caller's cache as the kernels take it, checked.
+vt_status kv_view(const vt_kv_cache* c, KvView& v) {
+    if (!c || !c->k || !c->v || (c->S > 0 && !c->pages) || (c->format != VT_KV_BF16 && c->format != VT_KV_E4M3)) return VT_ERR_INVALID_ARG;
+    const bool e4m3 = c->format == VT_KV_E4M3;
+    if (e4m3 != (c->k_exp != nullptr) || e4m3 != (c->v_exp != nullptr)) return VT_ERR_INVALID_ARG;
+    if (c->n_pages < 1 || c->heads < 1 || c->page < 1 || c->S < 0 || c->max_pages < 1 || c->pages_ld < c->max_pages) return VT_ERR_INVALID_ARG;
+    if ((int64_t)c->max_pages * c->page > INT32_MAX) return VT_ERR_INVALID_ARG;
+    if (!kv_head_size_ok(c->d) || c->heads > 1024) return VT_ERR_UNSUPPORTED;
+    const int64_t size = e4m3 ? 1 : 2, unit = 16 / size;
+    for (const int64_t s : {c->stride_page, c->stride_head, c->stride_token})
+        if (s < 1 || s % unit || s > INT64_MAX / 4) return VT_ERR_INVALID_ARG;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_exp, 16) || !aligned(c->v_exp, 16) || !aligned(c->pages, 4)) return VT_ERR_INVALID_ARG;
+    v = KvView{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_exp, c->v_exp, c->stride_page * size, c->stride_head * size,
+               c->stride_token * size, c->pages, c->pages_ld, c->n_pages, c->heads, c->page, c->d, c->S, c->max_pages};
+    return VT_OK;
+}
+
+// The control block of an optional workspace.
+vt_status kv_ctrl(void* ws, Ctrl*& ctrl) {
+    if (ws && !aligned(ws, 256)) return VT_ERR_WORKSPACE;
+    ctrl = static_cast<Ctrl*>(ws);
+    return VT_OK;
+}
+
 vt_status check_ws(void* ws, size_t ws_bytes, size_t need) {
     if (!ws || !aligned(ws, 256) || need == 0 || ws_bytes < need) return VT_ERR_WORKSPACE;
     return VT_OK;
@@ -111,6 +142,9 @@ size_t vt_workspace_bytes(int op, int64_t n, int32_t V, int32_t K, int32_t d, in
         case VT_OP_DRAFT_HEAD_HOST:
             if (!head_shape_ok(B, K, d, topk)) return 0;
             return host_stage(B, K, d, topk, VT_CTRL_BYTES + head_scratch(B, K, d, topk)).bytes;
+        case VT_OP_KV_ATTEND:
+            if (!kv_attend_shape_ok(n, B, K, V, d)) return 0;
+            return VT_CTRL_BYTES + kv_attend_scratch_bytes(B * (K / V), d);
         default:
             return 0;
     }
@@ -148,7 +182,7 @@ vt_status vt_read_status(void* ws, void* stream, uint32_t* flags, uint64_t* n_ba
     if (flags) *flags = host.flags;
     if (n_bad) *n_bad = host.n_bad;
     if (host.flags & VT_FLAG_TIMEOUT) return VT_ERR_TIMEOUT;
-    if (host.flags & (VT_FLAG_BAD_ID | VT_FLAG_BAD_MAP)) return VT_ERR_RANGE;
+    if (host.flags & (VT_FLAG_BAD_ID | VT_FLAG_BAD_MAP | VT_FLAG_BAD_PAGE)) return VT_ERR_RANGE;
     if (host.flags & (VT_FLAG_BAD_TEMP | VT_FLAG_NAN_ROW)) return VT_ERR_NUMERIC;
     return VT_OK;
 }
@@ -471,6 +505,100 @@ vt_status vt_draft_head_host(const uint16_t* h_host, const uint16_t* W_trim, con
     e = cudaMemcpyAsync(out_ids_host, di, out_bytes, cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaMemcpyAsync(out_logprobs_host, dl, out_bytes, cudaMemcpyDeviceToHost, s);
     return from_cuda(e);
+}
+
+vt_status vt_rope_freqs(int32_t rot, double base, double factor, double low_factor, double high_factor, double original, int64_t* freqs) {
+    if (!freqs || rot < 16 || rot > 256 || rot % 16 || !(base > 1.0) || !(factor >= 1.0) || !std::isfinite(base) || !std::isfinite(factor))
+        return VT_ERR_INVALID_ARG;
+    if (factor > 1.0 && (!(low_factor > 0.0) || !(high_factor > low_factor) || !(original > 0.0) || !std::isfinite(high_factor) || !std::isfinite(original)))
+        return VT_ERR_INVALID_ARG;
+    constexpr double two_pi = 6.283185307179586476925286766559;
+    for (int32_t i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (factor > 1.0) {
+            const double waves = original * f / two_pi;             // wavelengths in the original context
+            const double keep = (waves - low_factor) / (high_factor - low_factor);
+            if (keep <= 0.0) f /= factor;
+            else if (keep < 1.0) f *= (1.0 - keep) / factor + keep;
+        }
+        freqs[i] = (int64_t)std::llrint(std::ldexp(f / two_pi, 64));   // (f <= 1: under a quarter turn, 2^62)
+    }
+    return VT_OK;
+}
+
+vt_status vt_qkv_write(const uint16_t* q, int64_t q_ld, const uint16_t* k, int64_t k_ld, const uint16_t* v, int64_t v_ld, int32_t T,
+                       int32_t Hq, const vt_kv_cache* cache, const int32_t* seq, const int32_t* index, const int32_t* positions,
+                       const int64_t* freqs, int32_t rot, int32_t interleaved, const uint16_t* q_weight, const uint16_t* k_weight,
+                       double eps, uint16_t* q_out, void* ws, void* stream) {
+    KvWriteArgs a{};
+    vt_status st = kv_view(cache, a.c);
+    if (st != VT_OK) return st;
+    if ((st = kv_ctrl(ws, a.ctrl)) != VT_OK) return st;
+    if (T < 0 || Hq < 0 || Hq > 1024) return VT_ERR_INVALID_ARG;
+    if ((freqs != nullptr) != (rot > 0) || rot < 0 || rot > a.c.d || rot % 16 || !(eps >= 0.0) || !std::isfinite(eps)) return VT_ERR_INVALID_ARG;
+    if (T == 0) return VT_OK;
+    if ((Hq > 0) != (q != nullptr) || (Hq > 0 && !q_out)) return VT_ERR_INVALID_ARG;
+    if (!k || !v || !index || (freqs && !positions) || a.c.S < 1 || (!seq && T % a.c.S)) return VT_ERR_INVALID_ARG;
+    const int64_t least = (int64_t)a.c.heads * a.c.d;
+    if (k_ld < least || v_ld < least || (q && q_ld < (int64_t)Hq * a.c.d) || (k_ld | v_ld | (q ? q_ld : 0)) & 7) return VT_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16) ||
+        !aligned(seq, 4) || !aligned(index, 4) || !aligned(positions, 4) || !aligned(freqs, 8))
+        return VT_ERR_INVALID_ARG;
+    a.q = q, a.k = k, a.v = v, a.q_ld = q_ld, a.k_ld = k_ld, a.v_ld = v_ld, a.q_out = q_out, a.T = T, a.Hq = Hq;
+    a.seq = seq, a.index = index, a.positions = positions, a.freqs = freqs, a.rot = rot, a.interleaved = interleaved != 0;
+    a.q_weight = q_weight, a.k_weight = k_weight, a.eps = eps;
+    return from_cuda(launch_qkv_write(a, as_stream(stream)));
+}
+
+vt_status vt_kv_read(const vt_kv_cache* cache, const int32_t* seq, const int32_t* index, int32_t T, uint16_t* k_out, uint16_t* v_out, void* ws,
+                     void* stream) {
+    KvReadArgs a{};
+    vt_status st = kv_view(cache, a.c);
+    if (st != VT_OK) return st;
+    if ((st = kv_ctrl(ws, a.ctrl)) != VT_OK) return st;
+    if (T < 0) return VT_ERR_INVALID_ARG;
+    if (T == 0) return VT_OK;
+    if (!index || !k_out || !v_out || a.c.S < 1 || (!seq && T % a.c.S)) return VT_ERR_INVALID_ARG;
+    if (!aligned(seq, 4) || !aligned(index, 4) || !aligned(k_out, 16) || !aligned(v_out, 16)) return VT_ERR_INVALID_ARG;
+    a.seq = seq, a.index = index, a.T = T, a.k_out = k_out, a.v_out = v_out;
+    return from_cuda(launch_kv_read(a, as_stream(stream)));
+}
+
+vt_status vt_kv_attend(const uint16_t* q, int64_t q_ld, int32_t Q, int32_t Hq, const vt_kv_cache* cache, const int32_t* lens, const int32_t* node,
+                       const int32_t* parent, int64_t parent_ld, int32_t N, float scale, uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                       void* stream) {
+    KvAttendArgs a{};
+    vt_status st = kv_view(cache, a.c);
+    if (st != VT_OK) return st;
+    if (Q < 1 || Hq < 1 || Hq % a.c.heads || !std::isfinite(scale)) return VT_ERR_INVALID_ARG;
+    if (node && (N < 0 || (parent && parent_ld < N))) return VT_ERR_INVALID_ARG;
+    if (!kv_attend_shape_ok(a.c.S, Q, Hq, a.c.heads, a.c.d) || (node && N > VT_KV_MAX_NODES)) return VT_ERR_UNSUPPORTED;
+    if ((int64_t)a.c.S * Q > INT32_MAX) return VT_ERR_UNSUPPORTED;
+    st = check_ws(ws, ws_bytes, vt_workspace_bytes(VT_OP_KV_ATTEND, a.c.S, a.c.heads, Hq, a.c.d, Q, 0));
+    if (st != VT_OK) return st;
+    if (a.c.S == 0) return VT_OK;
+    if (!q || !lens || !out || q_ld < (int64_t)Hq * a.c.d || (q_ld & 7)) return VT_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lens, 4) || !aligned(node, 4) || !aligned(parent, 4) || !aligned(lse, 4)) return VT_ERR_INVALID_ARG;
+    a.q = q, a.q_ld = q_ld, a.Q = Q, a.Hq = Hq, a.group = Hq / a.c.heads, a.N = node ? N : 0;
+    a.lens = lens, a.node = node, a.parent = node ? parent : nullptr, a.parent_ld = parent_ld;
+    a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    a.out = out, a.lse = lse, a.ctrl = static_cast<Ctrl*>(ws);
+    kv_attend_carve(a, static_cast<uint8_t*>(ws) + VT_CTRL_BYTES);
+    return from_cuda(launch_kv_attend(a, as_stream(stream)));
+}
+
+vt_status vt_kv_commit(const vt_kv_cache* cache, const int32_t* lens, const int32_t* path, const int32_t* n_accept, const int32_t* nodes, int32_t N,
+                       int32_t* new_lens, void* ws, void* stream) {
+    KvCommitArgs a{};
+    vt_status st = kv_view(cache, a.c);
+    if (st != VT_OK) return st;
+    if ((st = kv_ctrl(ws, a.ctrl)) != VT_OK) return st;
+    if (N < 1) return VT_ERR_INVALID_ARG;
+    if (a.c.S == 0) return VT_OK;
+    if (!lens || !path || !n_accept) return VT_ERR_INVALID_ARG;
+    if (!aligned(lens, 4) || !aligned(path, 4) || !aligned(n_accept, 4) || !aligned(nodes, 4) || !aligned(new_lens, 4)) return VT_ERR_INVALID_ARG;
+    a.lens = lens, a.path = path, a.n_accept = n_accept, a.nodes = nodes, a.N = N, a.new_lens = new_lens;
+    return from_cuda(launch_kv_commit(a, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -9,6 +9,7 @@
 
 #include <ATen/ops/empty.h>
 
+#include <cmath>
 #include <cstdint>
 
 #include "vocabtrim.h"
@@ -21,6 +22,10 @@ decltype(&vt_tree_rerank) g_rerank;
 decltype(&vt_verify_greedy) g_verify;
 decltype(&vt_build_vocab) g_build;
 decltype(&vt_trim_head) g_trim;
+decltype(&vt_qkv_write) g_qkv_write;
+decltype(&vt_kv_read) g_kv_read;
+decltype(&vt_kv_attend) g_kv_attend;
+decltype(&vt_kv_commit) g_kv_commit;
 PyObject *g_make_ws, *g_raw_stream, *g_device;       // (op, shape, like) -> Workspace; torch's raw current stream of a device; its current device
 PyObject *s_ptr, *s_nbytes;
 
@@ -351,6 +356,233 @@ PyObject* trim_head(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the key-value cache ------------------------------------------------------------------------------------
+
+// Every tensor of these calls lies on the current device: the launch goes to its stream.
+const at::Tensor& on(PyObject* o, at::ScalarType dtype, const char* name, int64_t device) {
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.scalar_type() != dtype)
+        raise(PyExc_TypeError, "%s must be a CUDA tensor of dtype %s", name, c10::toString(dtype));
+    if (t.get_device() != device) raise(PyExc_ValueError, "%s must be on the current device", name);
+    return t;
+}
+const at::Tensor& flat(PyObject* o, at::ScalarType dtype, const char* name, int64_t device, int64_t count) {
+    const at::Tensor& t = on(o, dtype, name, device);
+    if (!t.is_contiguous()) raise(PyExc_TypeError, "%s must be contiguous", name);
+    if (t.numel() != count) raise(PyExc_ValueError, "%s must have %lld entries, not %lld", name, (long long)count, (long long)t.numel());
+    return t;
+}
+template <class T>
+T* flat_or_null(PyObject* o, at::ScalarType dtype, const char* name, int64_t device, int64_t count) {
+    return o == Py_None ? nullptr : data<T>(flat(o, dtype, name, device, count));
+}
+
+int64_t device_index() {
+    Ref d(PyObject_CallNoArgs(g_device));
+    if (!d.p) raise();
+    return integer(d.p);
+}
+
+int32_t fits_int(int64_t v, const char* name) {
+    if (v < 0 || v > INT32_MAX) raise(PyExc_ValueError, "%s is out of range", name);
+    return (int32_t)v;
+}
+
+// (k, v) or (k, v, k_exp, v_exp), and the page table
+struct Cache {
+    vt_kv_cache c{};
+    int64_t device;
+    Cache(PyObject* o, PyObject* table) : device(device_index()) {
+        const Ref seq(PySequence_Fast(o, "the cache must be (k, v) or (k, v, k_exp, v_exp)"));
+        if (!seq.p) raise();
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq.p);
+        if (n != 2 && n != 4) raise(PyExc_ValueError, "the cache must be (k, v) or (k, v, k_exp, v_exp)");
+        PyObject** at = PySequence_Fast_ITEMS(seq.p);
+        const at::ScalarType type = tensor(at[0]).scalar_type();
+        if (type != at::kBFloat16 && type != at::kFloat8_e4m3fn) raise(PyExc_TypeError, "the cache must hold bfloat16 or float8_e4m3fn");
+        const at::Tensor &k = on(at[0], type, "k cache", device), &v = on(at[1], type, "v cache", device);
+        if (k.dim() != 4 || v.dim() != 4 || k.sizes() != v.sizes()) raise(PyExc_ValueError, "k and v cache must both be [n_pages, heads, page, d]");
+        if (k.strides() != v.strides()) raise(PyExc_ValueError, "k and v cache must have the same strides");
+        if (k.stride(3) != 1) raise(PyExc_ValueError, "the cache's rows must be contiguous");
+        c.k = data<uint8_t>(k), c.v = data<uint8_t>(v);
+        c.n_pages = fits_int(k.size(0), "n_pages"), c.heads = fits_int(k.size(1), "heads"), c.page = fits_int(k.size(2), "page"), c.d = fits_int(k.size(3), "d");
+        // (a dim of one entry is never stepped over: its stride may be anything)
+        c.stride_page = c.n_pages > 1 ? k.stride(0) : c.d, c.stride_head = c.heads > 1 ? k.stride(1) : c.d, c.stride_token = c.page > 1 ? k.stride(2) : c.d;
+        if (type == at::kFloat8_e4m3fn) {
+            c.format = VT_KV_E4M3;
+            if (n != 4) raise(PyExc_ValueError, "a cache of float8_e4m3fn needs its exponents: (k, v, k_exp, v_exp)");
+            uint8_t** exps[] = {&c.k_exp, &c.v_exp};
+            for (int i = 0; i < 2; ++i) *exps[i] = data<uint8_t>(flat(at[2 + i], at::kByte, i ? "v_exp" : "k_exp", device, (int64_t)c.n_pages * c.heads * c.page));
+        } else if (n == 4 && (at[2] != Py_None || at[3] != Py_None)) raise(PyExc_ValueError, "a cache of bfloat16 has no exponents");
+        const at::Tensor& p = on(table, at::kInt, "pages", device);
+        if (p.dim() != 2 || (p.size(1) > 1 && p.stride(1) != 1)) raise(PyExc_ValueError, "pages must be [S, max_pages] with contiguous rows");
+        c.pages = data<int32_t>(p);
+        c.S = fits_int(p.size(0), "S"), c.max_pages = fits_int(p.size(1), "max_pages");
+        c.pages_ld = c.S > 1 ? p.stride(0) : c.max_pages;
+    }
+};
+
+// [T, heads, d] with heads side by side: the distance of its tokens
+int64_t token_stride(const at::Tensor& t, const char* name, int64_t T, int64_t d) {
+    if (t.dim() != 3 || (T >= 0 && t.size(0) != T) || t.size(2) != d) raise(PyExc_ValueError, "%s must be [T, heads, d]", name);
+    if (t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != d)) raise(PyExc_ValueError, "%s must have its heads side by side", name);
+    return t.size(0) > 1 ? t.stride(0) : t.size(1) * d;
+}
+
+void* control(PyObject* ws) {                        // of an optional workspace
+    if (ws == Py_None) return nullptr;
+    Ref p(PyObject_GetAttr(ws, s_ptr));
+    if (!p.p) raise();
+    return pointer(p.p);
+}
+
+// (q or None, k, v, cache, pages, index, seq, positions, freqs, q_weight, k_weight, eps, interleaved, out, ws)
+PyObject* qkv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect_args(n, 15);
+    const Cache cache(a[3], a[4]);
+    const int64_t dev = cache.device, d = cache.c.d, heads = cache.c.heads;
+    const at::Tensor &k = on(a[1], at::kBFloat16, "k", dev), &v = on(a[2], at::kBFloat16, "v", dev);
+    const int64_t k_ld = token_stride(k, "k", -1, d), T = k.size(0), v_ld = token_stride(v, "v", T, d);
+    if (k.size(1) != heads || v.size(1) != heads) raise(PyExc_ValueError, "k and v must have the cache's %lld heads", (long long)heads);
+    int64_t q_ld = 0, Hq = 0;
+    const uint16_t* q = nullptr;
+    Ref out;
+    if (a[0] != Py_None) {
+        const at::Tensor& t = on(a[0], at::kBFloat16, "q", dev);
+        q_ld = token_stride(t, "q", T, d), Hq = t.size(1), q = data<uint16_t>(t);
+        if (a[13] == Py_None) out.p = THPVariable_Wrap(make(t, at::kBFloat16, {T, Hq, d}));
+        else Py_INCREF(out.p = a[13]);
+        if (!out.p) raise();
+    } else Py_INCREF(out.p = Py_None);
+    uint16_t* q_out = a[0] != Py_None ? data<uint16_t>(flat(out.p, at::kBFloat16, "out", dev, T * Hq * d)) : nullptr;
+    const int32_t *index = data<int32_t>(flat(a[5], at::kInt, "index", dev, T)), *seq = flat_or_null<int32_t>(a[6], at::kInt, "seq", dev, T);
+    const int32_t* positions = flat_or_null<int32_t>(a[7], at::kInt, "positions", dev, T);
+    int64_t rot = 0;
+    const int64_t* freqs = nullptr;
+    if (a[8] != Py_None) {
+        const at::Tensor& t = on(a[8], at::kLong, "freqs", dev);
+        if (!t.is_contiguous()) raise(PyExc_TypeError, "freqs must be contiguous");
+        freqs = data<int64_t>(t), rot = 2 * t.numel();
+        if (a[7] == Py_None) raise(PyExc_ValueError, "a rotation needs positions");
+        if (rot < 16 || rot > d || rot % 16) raise(PyExc_ValueError, "freqs must have 8, 16, ... d / 2 entries");
+    }
+    if (!seq && T && (!cache.c.S || T % cache.c.S)) raise(PyExc_ValueError, "without seq, every sequence must have the same number of rows");
+    const uint16_t *qw = flat_or_null<uint16_t>(a[9], at::kBFloat16, "q_weight", dev, d), *kw = flat_or_null<uint16_t>(a[10], at::kBFloat16, "k_weight", dev, d);
+    const double eps = PyFloat_AsDouble(a[11]);
+    if (eps == -1.0 && PyErr_Occurred()) raise();
+    const int interleaved = PyObject_IsTrue(a[12]);
+    if (interleaved < 0) raise();
+    void* ws = control(a[14]);
+    void* s = stream();
+    const int status = call(g_qkv_write, q, q_ld, data<uint16_t>(k), k_ld, data<uint16_t>(v), v_ld, fits_int(T, "T"), fits_int(Hq, "q's heads"), &cache.c,
+                            seq, index, positions, freqs, (int32_t)rot, (int32_t)interleaved, qw, kw, eps, q_out, ws, s);
+    if (status != VT_OK) return PyLong_FromLong(status);
+    Py_INCREF(out.p);
+    return out.p;
+    END_HANDLE_TH_ERRORS
+}
+
+// (cache, pages, index, seq, out, ws)
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect_args(n, 6);
+    const Cache cache(a[0], a[1]);
+    const at::Tensor& index = on(a[2], at::kInt, "index", cache.device);
+    if (!index.is_contiguous()) raise(PyExc_TypeError, "index must be contiguous");
+    const int64_t T = index.numel(), count = T * cache.c.heads * cache.c.d;
+    const int32_t* seq = flat_or_null<int32_t>(a[3], at::kInt, "seq", cache.device, T);
+    if (!seq && T && (!cache.c.S || T % cache.c.S)) raise(PyExc_ValueError, "without seq, every sequence must have the same number of rows");
+    Ref k, v;
+    if (a[4] == Py_None) {
+        k.p = THPVariable_Wrap(make(index, at::kBFloat16, {T, cache.c.heads, cache.c.d}));
+        v.p = THPVariable_Wrap(make(index, at::kBFloat16, {T, cache.c.heads, cache.c.d}));
+        if (!k.p || !v.p) raise();
+    } else {
+        Parts p(a[4], 2);
+        Py_INCREF(k.p = p.at[0]);
+        Py_INCREF(v.p = p.at[1]);
+    }
+    uint16_t *ko = data<uint16_t>(flat(k.p, at::kBFloat16, "k out", cache.device, count)), *vo = data<uint16_t>(flat(v.p, at::kBFloat16, "v out", cache.device, count));
+    void* ws = control(a[5]);
+    void* s = stream();
+    const int status = call(g_kv_read, &cache.c, seq, data<int32_t>(index), fits_int(T, "T"), ko, vo, ws, s);
+    if (status != VT_OK) return PyLong_FromLong(status);
+    return PyTuple_Pack(2, k.p, v.p);
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, cache, pages, lens, node, parent, scale or None, out, ws)
+PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect_args(n, 9);
+    const Cache cache(a[1], a[2]);
+    const int64_t dev = cache.device, d = cache.c.d, S = cache.c.S;
+    const at::Tensor& q = on(a[0], at::kBFloat16, "q", dev);
+    const int64_t q_ld = token_stride(q, "q", -1, d), T = q.size(0), Hq = q.size(1);
+    if (S ? (T == 0 || T % S) : T != 0) raise(PyExc_ValueError, "q must have the same number of rows for each of the %lld sequences", (long long)S);
+    if (Hq < 1 || Hq % cache.c.heads) raise(PyExc_ValueError, "q's heads must be a multiple of the cache's");
+    const int64_t Q = S ? T / S : 1;
+    const int32_t* lens = data<int32_t>(flat(a[3], at::kInt, "lens", dev, S));
+    const int32_t *node = flat_or_null<int32_t>(a[4], at::kInt, "node", dev, T), *parent = nullptr;
+    int64_t N = a[4] != Py_None ? VT_KV_MAX_NODES : 0, parent_ld = 0;
+    if (a[5] != Py_None) {
+        const at::Tensor& p = on(a[5], at::kInt, "parent", dev);
+        if (a[4] == Py_None) raise(PyExc_ValueError, "parent needs node");
+        if (p.dim() != 2 || p.size(0) != S || (p.size(1) > 1 && p.stride(1) != 1)) raise(PyExc_ValueError, "parent must be [S, N] with contiguous rows");
+        N = p.size(1), parent_ld = S > 1 ? p.stride(0) : N, parent = data<int32_t>(p);
+    }
+    double scale = 0.0;
+    if (a[6] != Py_None) {
+        scale = PyFloat_AsDouble(a[6]);
+        if (scale == -1.0 && PyErr_Occurred()) raise();
+    } else scale = 1.0 / std::sqrt((double)d);
+    Ref out, lse;
+    if (a[7] == Py_None) {
+        out.p = THPVariable_Wrap(make(q, at::kBFloat16, {T, Hq, d}));
+        lse.p = THPVariable_Wrap(make(q, at::kFloat, {T, Hq}));
+        if (!out.p || !lse.p) raise();
+    } else {
+        Parts p(a[7], 2);
+        Py_INCREF(out.p = p.at[0]);
+        Py_INCREF(lse.p = p.at[1]);
+    }
+    uint16_t* o = data<uint16_t>(flat(out.p, at::kBFloat16, "out", dev, T * Hq * d));
+    float* l = data<float>(flat(lse.p, at::kFloat, "lse", dev, T * Hq));
+    fits_int(Q, "rows"), fits_int(Hq, "q's heads"), fits_int(N, "nodes");
+    const Space ws(a[8], VT_OP_KV_ATTEND, a[0], S, cache.c.heads, Hq, d, Q, 0);
+    void* s = stream();
+    const int status = call(g_kv_attend, data<uint16_t>(q), q_ld, (int32_t)Q, (int32_t)Hq, &cache.c, lens, node, parent, parent_ld, (int32_t)N,
+                            (float)scale, o, l, ws.ptr, ws.bytes, s);
+    if (status != VT_OK) return PyLong_FromLong(status);
+    return PyTuple_Pack(2, out.p, lse.p);
+    END_HANDLE_TH_ERRORS
+}
+
+// (cache, pages, lens, path, n_accept, nodes, out, ws)
+PyObject* kv_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect_args(n, 8);
+    const Cache cache(a[0], a[1]);
+    const int64_t dev = cache.device, S = cache.c.S;
+    const at::Tensor &lens = flat(a[2], at::kInt, "lens", dev, S), &path = on(a[3], at::kInt, "path", dev);
+    if (path.dim() != 2 || path.size(0) != S || !path.is_contiguous()) raise(PyExc_ValueError, "path must be a contiguous [S, N]");
+    const int64_t N = path.size(1);
+    const int32_t *accepted = data<int32_t>(flat(a[4], at::kInt, "n_accept", dev, S)), *nodes = flat_or_null<int32_t>(a[5], at::kInt, "nodes", dev, S * N);
+    Ref out;
+    if (a[6] == Py_None) out.p = THPVariable_Wrap(make(lens, at::kInt, {S}));
+    else Py_INCREF(out.p = a[6]);
+    if (!out.p) raise();
+    int32_t* fresh = data<int32_t>(flat(out.p, at::kInt, "out", dev, S));
+    void* ws = control(a[7]);
+    void* s = stream();
+    const int status = call(g_kv_commit, &cache.c, data<int32_t>(lens), data<int32_t>(path), accepted, nodes, fits_int(N, "N"), fresh, ws, s);
+    if (status != VT_OK) return PyLong_FromLong(status);
+    Py_INCREF(out.p);
+    return out.p;
+    END_HANDLE_TH_ERRORS
+}
+
 // (addresses of the library's functions by name, make_ws, raw_stream, current_device)
 PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -368,6 +600,10 @@ PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_verify = reinterpret_cast<decltype(g_verify)>(at("vt_verify_greedy"));
     g_build = reinterpret_cast<decltype(g_build)>(at("vt_build_vocab"));
     g_trim = reinterpret_cast<decltype(g_trim)>(at("vt_trim_head"));
+    g_qkv_write = reinterpret_cast<decltype(g_qkv_write)>(at("vt_qkv_write"));
+    g_kv_read = reinterpret_cast<decltype(g_kv_read)>(at("vt_kv_read"));
+    g_kv_attend = reinterpret_cast<decltype(g_kv_attend)>(at("vt_kv_attend"));
+    g_kv_commit = reinterpret_cast<decltype(g_kv_commit)>(at("vt_kv_commit"));
     PyObject** kept[] = {&g_make_ws, &g_raw_stream, &g_device};
     for (int i = 0; i < 3; ++i) {
         Py_INCREF(a[1 + i]);
@@ -380,7 +616,7 @@ PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define VT_FN(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VT_FN(draft_head), VT_FN(draft_head_expand), VT_FN(draft_head_host), VT_FN(tree_rerank), VT_FN(verify_greedy),
-                           VT_FN(build_vocab), VT_FN(trim_head), VT_FN(use), {nullptr, nullptr, 0, nullptr}};
+                           VT_FN(build_vocab), VT_FN(trim_head), VT_FN(qkv_write), VT_FN(kv_read), VT_FN(kv_attend), VT_FN(kv_commit), VT_FN(use), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_vt_bind", "Argument marshalling for libvocabtrim.so", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
