@@ -9,7 +9,7 @@ namespace vt {
 
 constexpr int kKvMaxNew = VT_KV_MAX_NEW;         // new rows of a sequence in one attention call: bits of a node's row mask
 constexpr int kKvMaxNodes = VT_KV_MAX_NODES;     // nodes of a sequence's tree
-constexpr int kKvMaxCtas = 592;                  // CTAs of the attention kernel (four on each of 148 SMs): its workspace holds two partial results of each
+constexpr int kKvMaxCtas = 160;                  // CTAs of the attention kernel (one an SM): its workspace holds two partial results of each
 
 // A cache and its page table as the kernels take them (strides in bytes).
 struct KvView {
@@ -63,6 +63,7 @@ struct KvAttendArgs {
     int32_t Q, Hq, group, N;      // rows a sequence, query heads (and those of a key head), nodes a sequence
     const int32_t *lens, *node, *parent;
     int64_t parent_ld;
+    int32_t page_shift, box;      // log2 of the page where it is a power of two, else -1; tokens of a tensor copy: 32, 16 or (other pages) 0
     float scale_log2;             // the scores' scale times log2(e)
     uint16_t* out;                // [S * Q, Hq, d]
     float* lse;                   // [S * Q, Hq], or nullptr
@@ -71,7 +72,7 @@ struct KvAttendArgs {
     int32_t part_rows;
     Ctrl* ctrl;
 };
-int kv_attend_warp_rows(int rows);               // warps side by side over a key head's rows (1, 2 or 4 of 16 rows each)
+int kv_attend_warp_rows(int rows, int d);        // warps side by side over a key head's rows (1, 2 or 4 of 16 rows each)
 size_t kv_attend_scratch_bytes(int rows, int d);
 cudaError_t launch_kv_attend_bf16(const KvAttendArgs& a, int& ctas, cudaStream_t s);
 cudaError_t launch_kv_attend_e4m3(const KvAttendArgs& a, int& ctas, cudaStream_t s);

@@ -13,62 +13,111 @@
 // delivers it), and it keeps scores and weights in registers, where tcgen05 would send both through TMEM for tiles of 128 rows that
 // are seven eighths empty.
 //
-// Split: the work is cut into units of 16 * WR tokens, in the order (sequence, key head, group of rows, tokens), and every CTA takes an equal run of
+// Split: the work is cut into units of 64 tokens, in the order (sequence, key head, group of rows, tokens), and every CTA takes an equal run of
 // units, whatever the lengths are; nothing is known to the host, so a captured graph stays right when lengths change.  A (sequence, head, group)
 // whose units lie in several CTAs leaves partial results, which a second launch joins in the order of the tokens.
 //
-// Teams: the CTA's four warps are 4 / WR teams.  A team has a ring of its own in shared memory, filled by cp.async, and takes every
-// (4 / WR)-th unit: no barrier of the whole CTA while tokens stream.
+// Roles: four producer warps walk the CTA's run, look pages up, and fill rings of tiles by tensor copies of 16 tokens, as far ahead as the rings reach
+// (copies of a row each took 10 ns apiece, twice what there is); eight warps consume, as 8 / WR teams that take the tiles in turn.  So the copies go on while a result is finished and the next one's queries are
+// fetched, which took 5 us a result when the same warps did both.
 #pragma once
+#include <cuda_fp16.h>
+
 #include "vt_kv.cuh"
+#include "vt_maps.cuh"
+#include "vt_mbar.cuh"
 
 namespace vt {
 namespace {
 
-constexpr int kAttThreads = 128;
+constexpr int kAttWarps = 8;                                     // that consume
+constexpr int kAttFeeds = 4;                                     // that produce
+constexpr int kAttThreads = 32 * (kAttWarps + kAttFeeds);
+// Registers: 168 of each thread at the launch are 2016 of each lane; the consumers take 200, which leaves the producers 104.
+constexpr int kAttConsumerRegs = 200, kAttProducerRegs = 104;
+static_assert(kAttWarps * kAttConsumerRegs + kAttFeeds * kAttProducerRegs <= (kAttWarps + kAttFeeds) * 168, "what the block was launched with");
+constexpr int kAttUnit = 64;                                     // tokens
+constexpr int kAttTreeUnits = 2;                                 // what a tree's tokens count for when the work is dealt out
+constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
+constexpr int kAttRound = kAttTile * kAttFeeds;                  // tokens that the producers look up at a time
+constexpr unsigned long long kAttWaitNs = 2000000000ull;         // bound of a wait on a tile or a place in the ring
 
 template <int D, bool F8, int WR>
 struct AttCfg {
-    static constexpr int kTeams = 4 / WR;
-    static constexpr int kTile = 16 * WR;                        // tokens of a unit
+    static constexpr int kTeams = kAttWarps / WR;
+    static constexpr int kTile = kAttTile;
     static constexpr int kRow = D * (F8 ? 1 : 2);                // bytes of a cached row
-    static constexpr int kPitch = kRow + 16;                     // an odd number of 16-byte vectors: ldmatrix meets no bank twice
-    static constexpr int kHalf = kTile * kPitch;
-    static constexpr int kStage = 2 * kHalf + (F8 ? 2 * kTile : 0);   // keys, values, their exponents
-    static constexpr int kCtaStage = kTeams * kStage;            // (64 tokens, whatever WR is)
-    static constexpr int kStages = F8 ? (D > 128 ? 3 : 4) : (D > 192 ? 2 : 3);
-    static constexpr int kRing = kStages * kCtaStage;
+    // A tile lies in shared memory as tensor copies write it: blocks of kBox bytes of all its rows, the 16-byte vectors of a row swapped by the
+    // copies' swizzle of that width, so that ldmatrix meets no bank twice.
+    static constexpr int kBox = kRow % 128 == 0 ? 128 : kRow % 64 == 0 ? 64 : 32;
+    static constexpr int kHalf = kTile * kRow;
+    static constexpr int kSlot = 2 * kHalf;                      // keys, values
+    static constexpr int kToken = F8 ? 16 : 4;                   // what a tile holds of a token besides its rows
+    static constexpr int kMasks = kTile * kToken;                // the rows that see a tree's token, 8 bytes each
+    static constexpr int kHeader = kMasks + kTile * 8;
+    static constexpr int kNote = kHeader + 16;
     static constexpr bool kQRegs = D <= 128;                     // query fragments stay in registers
     static constexpr int kQPitch = 2 * D + 16;
     static constexpr int kQBytes = kQRegs ? 0 : WR * 16 * kQPitch;
-    static constexpr int kSmem = kRing + kQBytes;
-    static constexpr int kOPitch = D + 4;                        // floats of a row where the teams' results meet
-    static_assert(kTeams * 16 * WR * kOPitch * 4 <= kRing, "the teams' results fit the ring");
-    static_assert(kKvMaxNodes * 14 <= kRing - kCtaStage, "a tree's masks, list and parents fit behind the first stage");
-    static_assert(kRow % 32 == 0 && kSmem <= 227 * 1024, "shapes");
-};
+    static constexpr int kMeet = kAttWarps / 2 * (D / 8 + 1) * 512;   // where the teams' results meet: D / 8 + 1 vectors of each lane of half of them
+    static constexpr int kParents = 2 * kKvMaxNodes;
+    static constexpr int kFree = 226 * 1024 - 2048 - kQBytes - kMeet - kParents;
+    // A ring of kPer places for each producer.  Its tiles go to the teams in turn, and a place is always of the same team: who waits for a turn
+    // of a place has waited for every turn before, and cannot take the next but one, of the same parity, for its own.
+    static constexpr int kShare = kTeams > kAttFeeds ? kTeams / kAttFeeds : 1;             // teams of a ring
+    static constexpr int kPer = (kFree / (kSlot + kNote) < 40 ? kFree / (kSlot + kNote) : 40) / kAttFeeds / kShare * kShare;
+    static constexpr int kSlots = kAttFeeds * kPer;
+    static constexpr int kSmem = kSlots * (kSlot + kNote) + kQBytes + kMeet + kParents + 1024;     // (and what brings the ring to 1024)
+    static_assert(kPer >= kShare, "a place for each team");
+    static_assert(kRow % 32 == 0 && kSlot % 1024 == 0 && kNote % 16 == 0, "shapes");
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes, or zeros where `have` is false (then the source is not read)
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool have) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
+    __device__ static __forceinline__ uint32_t swizzle(uint32_t row) { return kBox == 128 ? row & 7 : kBox == 64 ? (row >> 1) & 3 : (row >> 2) & 1; }
+    __device__ static __forceinline__ uint32_t place(uint32_t row, uint32_t vec) {         // of a row's 16-byte vector in half a tile
+        constexpr uint32_t kVecs = kBox / 16;
+        return vec / kVecs * (kTile * kBox) + row * kBox + ((vec % kVecs ^ swizzle(row)) << 4);
+    }
+};
+// What an e4m3 tile holds of a token (bf16: the second alone): the factor of its score, 0 or (no such token) -inf to be added, the
+// exponent of its values within what keeps all weights finite, and their power of two (0: no such token).
+enum { kAttEnd = 1, kAttEmpty = 2, kAttTree = 4 };               // a tile's header
+
+// One lane of a converged warp: the compiler then knows that one thread is active.
+__device__ __forceinline__ bool elect_lane() {
+    uint32_t r;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+    return r != 0;
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// a box of the cache's map: dim x, token, head, page
+__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap* map, int x, int token, int head, int page, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(smem_u32(bar)) : "memory");
+}
+// orders this thread's stores to shared memory in front of later bulk copies into the same place
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void ldsm(uint32_t* r, uint32_t a) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
 __device__ __forceinline__ void ldsm_t(uint32_t* r, uint32_t a) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
+template <bool F16>
 __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    if (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float exp2_fast(float x) {            // ex2.approx: 2 ulp; weights below 2^-126 are zero
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float exp2_whole(float x) {           // with results below 2^-126
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -76,16 +125,30 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Four e4m3 bytes as two pairs of bf16: bytes 0 and 2, bytes 1 and 3.  Sign, exponent and mantissa bits are moved to bf16's places, which
-// gives the value times 2^-120 (subnormal ones too), and one exact multiplication puts it right.
-__device__ __forceinline__ uint32_t times_2_120(uint32_t x) {
-    uint32_t y;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(x), "r"(0x7b807b80u));
-    return y;
+// Four e4m3 bytes as two pairs of f16 (exact).  In a tree's tile (FINITE) by their bits, moved to f16's places, which is the value times
+// 2^-8, and one exact multiplication: a NaN byte then is a number, and a weight of zero keeps it out of the rows that do not see it.
+template <bool FINITE>
+__device__ __forceinline__ void e4m3_pairs(uint32_t x, uint32_t& lo, uint32_t& hi) {
+    if (FINITE) {
+        const uint32_t a = __byte_perm(x, 0, 0x1404), b = __byte_perm(x, 0, 0x3424);
+        const uint32_t c = (a & 0x80008000u) | ((a >> 1) & 0x3f803f80u), d = (b & 0x80008000u) | ((b >> 1) & 0x3f803f80u);
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(c), "r"(0x5c005c00u));
+        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(d), "r"(0x5c005c00u));
+    } else {
+        asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.f16x2.e4m3x2 %0, a; cvt.rn.f16x2.e4m3x2 %1, b; }" : "=r"(lo), "=r"(hi) : "r"(x));
+    }
 }
-__device__ __forceinline__ void e4m3_pairs(uint32_t x, uint32_t& even, uint32_t& odd) {
-    even = times_2_120(((x << 8) & 0x80008000u) | ((x << 4) & 0x07f007f0u));
-    odd = times_2_120((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u));
+
+// 2^k by its bits, k clamped to what fp32 holds
+__device__ __forceinline__ float two_to(int k) { return __uint_as_float((uint32_t)(min(max(k, -126), 127) + 127) << 23); }
+
+// A query row goes into f16 under the power of two that brings its largest magnitude to [2^14, 2^15): eight significant bits fit, and
+// what underflows is 2^-39 of the largest.  From the largest's bits: the power.
+__device__ __forceinline__ int q_power(uint32_t top_bits) { return min(14 + 127 - (int)(top_bits >> 23), 120); }
+// two bf16 as f16 times 2^k
+__device__ __forceinline__ uint32_t q_pair(uint32_t w, float f) {
+    const __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 template <int WR>
@@ -93,12 +156,30 @@ __device__ __forceinline__ void team_barrier(int team) {
     if (WR == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(32 * WR) : "memory");
 }
+__device__ __forceinline__ void consumers_barrier() { asm volatile("bar.sync 15, %0;" ::"n"(32 * kAttWarps) : "memory"); }
+
+__device__ __forceinline__ void feeds_barrier() { asm volatile("bar.sync 14, %0;" ::"n"(32 * kAttFeeds) : "memory"); }
+
+// A wait within the CTA (nothing here waits for another).  Where it runs out, the flag makes all later waits return at once, every loop still
+// ends, and the results are no numbers.
+__device__ __forceinline__ void att_wait(uint64_t* bar, uint32_t parity, volatile int* dead, Ctrl* ctrl) {
+    if (mbar_try(bar, parity)) return;
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try(bar, parity)) {
+        if (*dead) return;
+        if (global_ns() - t0 > kAttWaitNs) {
+            *dead = 1;
+            atomicOr(&ctrl->flags, (uint32_t)VT_FLAG_TIMEOUT);
+            return;
+        }
+    }
+}
 
 // What a warp keeps of its 16 rows: lane holds rows lane / 4 and lane / 4 + 8.
 template <int D>
 struct AttAcc {
     float o[D / 8][4];
-    float m[2], l[2];
+    float m[2], l[2];             // e4m3: m is the maximum of score plus the values' exponent
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
@@ -107,25 +188,22 @@ struct AttAcc {
     }
 };
 
-// The first dim of accumulator tile nt's pair for a lane, and the distance between its two dims.
-template <bool F8>
-__device__ __forceinline__ int o_dim(int nt, int j) { return F8 ? 16 * (nt >> 1) + 4 * j + (nt & 1) : 8 * nt + 2 * j; }
-
-// One unit: scores of the warp's 16 rows with the tile's tokens, running maximum, weighted values.  `seen`: the tile's tokens that
-// exist, as bits; LIST: tokens are entries of a tree's list, and `mask` says which new rows see each.
+// One tile: scores of the warp's 16 rows with its tokens, running maximum, weighted values.  LIST: tokens are a tree's nodes, and the
+// tile's masks say which new rows see each.
 template <int D, bool F8, int WR, bool LIST>
-__device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, uint8_t* stage, const uint64_t seen,
-                                         float scale, const unsigned long long* mask, int qi0, int qi1) {
+__device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, uint8_t* slot, const uint8_t* note, const float (&scale)[2],
+                                         int qi0, int qi1) {
     using C = AttCfg<D, F8, WR>;
-    constexpr int NT = 2 * WR;                                   // tiles of 8 tokens
-    constexpr uint64_t kAll = WR == 4 ? ~0ull : (1ull << (16 * WR % 64)) - 1;
+    constexpr int NT = C::kTile / 8;                             // groups of 8 tokens
     const int lane = threadIdx.x & 31, j = lane & 3;
     float s[NT][4];
 #pragma unroll
     for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
-    const uint32_t base = smem_addr(stage);
-    const uint32_t krow = base + ((lane >> 4) * 8 + (lane & 7)) * C::kPitch + ((lane >> 3) & 1) * 16;
-    constexpr int KS = D / (F8 ? 32 : 16);                       // 32 bytes of a row at a time
+    const uint32_t base = smem_u32(slot);
+    // ldmatrix: the lane's row, and the place of its vector there, but for the step's even number of vectors
+    constexpr uint32_t kVecs = C::kBox / 16;
+    const uint32_t k_row = (lane >> 4) * 8 + (lane & 7), k_at = base + k_row * C::kBox, k_vec = (((lane >> 3) & 1) ^ C::swizzle(k_row)) << 4;
+    constexpr int KS = C::kRow / 32;                             // 32 bytes of a row at a time
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         uint32_t qa[F8 ? 2 : 1][4];
@@ -140,66 +218,61 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
             }
         }
 #pragma unroll
-        for (int g = 0; g < WR; ++g) {
+        for (int g = 0; g < C::kTile / 16; ++g) {
             uint32_t b[4];
-            ldsm(b, krow + g * 16 * C::kPitch + ks * 32);
+            ldsm(b, k_at + (k_vec ^ (2 * ks % kVecs << 4)) + 2 * ks / kVecs * (C::kTile * C::kBox) + g * 16 * C::kBox);
             if (!F8) {
-                mma(s[2 * g], qa[0], b[0], b[1]);
-                mma(s[2 * g + 1], qa[0], b[2], b[3]);
+                mma<false>(s[2 * g], qa[0], b[0], b[1]);
+                mma<false>(s[2 * g + 1], qa[0], b[2], b[3]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {                    // i: (token half, dim half)
-                    uint32_t even, odd;
-                    e4m3_pairs(b[i], even, odd);
-                    mma(s[2 * g + (i >> 1)], qa[i & 1], even, odd);
+                    uint32_t lo, hi;
+                    e4m3_pairs<LIST>(b[i], lo, hi);
+                    mma<true>(s[2 * g + (i >> 1)], qa[i & 1], lo, hi);
                 }
             }
         }
     }
-    const uint8_t* exps = stage + 2 * C::kHalf;
+    // scores in base 2; what they stand against (the reference) is their maximum, of e4m3 with the exponent of the token's values on top, so
+    // that weight times power of two fits f16 whatever the powers are
+    float top[2] = {-INFINITY, -INFINITY}, vf[NT][2];
+    uint32_t sees[2] = {0, 0};                                   // LIST: bit 2 i + u: the row sees token 8 i + 2 j + u
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        float f0 = scale, f1 = scale;
-        if (F8) {
-            const uint32_t e = *reinterpret_cast<const uint16_t*>(exps + 8 * i + 2 * j);
-            f0 *= kv_two_to(e & 255u);
-            f1 *= kv_two_to(e >> 8);
-        }
-        s[i][0] *= f0, s[i][1] *= f1, s[i][2] *= f0, s[i][3] *= f1;
-    }
-    uint32_t sees[2] = {0, 0};                                   // bit 2 i + u: the row sees token 8 i + 2 j + u
-    const bool partial = LIST || seen != kAll;
-    if (partial) {
+        float ve[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int t = 8 * i + 2 * j + u;
-                const bool have = (seen >> t) & 1;
-                bool r0 = have, r1 = have;
-                if (LIST && have) {
-                    const unsigned long long bits = mask[t];
-                    r0 = (bits >> qi0) & 1, r1 = (bits >> qi1) & 1;
-                }
+        for (int u = 0; u < 2; ++u) {
+            const int t = 8 * i + 2 * j + u;
+            float bias;
+            if (F8) {
+                const float4 x = *reinterpret_cast<const float4*>(note + 16 * t);
+                s[i][u] *= x.x, s[i][2 + u] *= x.x;
+                bias = x.y, ve[u] = x.z, vf[i][u] = x.w;
+            } else {
+                bias = *reinterpret_cast<const float*>(note + 4 * t);
+            }
+            s[i][u] = fmaf(s[i][u], scale[0], bias), s[i][2 + u] = fmaf(s[i][2 + u], scale[1], bias);
+            if (LIST) {
+                const unsigned long long bits = *reinterpret_cast<const unsigned long long*>(note + C::kMasks + 8 * t);
+                const bool r0 = (bits >> qi0) & 1, r1 = (bits >> qi1) & 1;
                 sees[0] |= (uint32_t)r0 << (2 * i + u), sees[1] |= (uint32_t)r1 << (2 * i + u);
                 if (!r0) s[i][u] = -INFINITY;
                 if (!r1) s[i][2 + u] = -INFINITY;
             }
+            top[0] = fmaxf(top[0], s[i][u] + ve[u]), top[1] = fmaxf(top[1], s[i][2 + u] + ve[u]);
+        }
     }
-    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        top[0] = fmaxf(top[0], fmaxf(s[i][0], s[i][1]));
-        top[1] = fmaxf(top[1], fmaxf(s[i][2], s[i][3]));
-    }
+    bool grows = false;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
         top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+        grows |= top[r] > acc.m[r] + 4.0f;
     }
-    // The kept maximum may lie up to 4 below the true one (weights up to 16): results are divided by the sum of the same weights,
+    // The kept reference may lie up to 4 below the true one (weights up to 16): results are divided by the sum of the same weights,
     // and most tiles need not scale what is there.
-    if (__any_sync(0xffffffffu, top[0] > acc.m[0] + 4.0f || top[1] > acc.m[1] + 4.0f)) {
+    if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const float m = fmaxf(acc.m[r], top[r]);
@@ -217,24 +290,23 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
         s[i][2] = exp2_fast(s[i][2] - m1), s[i][3] = exp2_fast(s[i][3] - m1);
         acc.l[0] += s[i][0] + s[i][1];
         acc.l[1] += s[i][2] + s[i][3];
-        if (F8) {                                                // the values' powers of two go into the weights (exact)
-            const uint32_t e = *reinterpret_cast<const uint16_t*>(exps + C::kTile + 8 * i + 2 * j);
-            const float f0 = kv_two_to(e & 255u), f1 = kv_two_to(e >> 8);
-            s[i][0] *= f0, s[i][1] *= f1, s[i][2] *= f0, s[i][3] *= f1;
-            if (partial) {                                       // (what lies in an unseen place may be no number)
+        if (F8) {
+            s[i][0] *= vf[i][0], s[i][1] *= vf[i][1], s[i][2] *= vf[i][0], s[i][3] *= vf[i][1];
+            if (LIST) {                                          // (a power of a row that held a NaN is one)
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
                     if (!((sees[u >> 1] >> (2 * i + (u & 1))) & 1)) s[i][u] = 0.0f;
             }
         }
     }
-    uint8_t* vals = stage + C::kHalf;
+    uint8_t* vals = slot + C::kHalf;
     if (LIST && !F8) {
         // A drafted token that some of the rows see stays out of the others' sums by a weight of zero, and zero times an infinity or a NaN is
         // a NaN.  Such values are added to the rows that see them one by one, and are zeros for the MMA.
+        const int team = (int)(threadIdx.x >> 5) / WR;
         bool odd = false;
         for (int x = lane; x < C::kTile * (D / 8); x += 32) {
-            const uint4 w = *reinterpret_cast<const uint4*>(vals + (x / (D / 8)) * C::kPitch + (x % (D / 8)) * 16);
+            const uint4 w = *reinterpret_cast<const uint4*>(vals + C::place(x / (D / 8), x % (D / 8)));
             const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) odd |= (ws[i] & 0x7f80u) == 0x7f80u || (ws[i] & 0x7f800000u) == 0x7f800000u;
@@ -249,12 +321,11 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                         const float p0 = __shfl_sync(0xffffffffu, s[i][u], from), p1 = __shfl_sync(0xffffffffu, s[i][2 + u], from);
                         const bool r0 = (__shfl_sync(0xffffffffu, sees[0], from) >> (2 * i + u)) & 1;
                         const bool r1 = (__shfl_sync(0xffffffffu, sees[1], from) >> (2 * i + u)) & 1;
-                        const uint16_t* row = reinterpret_cast<const uint16_t*>(vals + (8 * i + t + u) * C::kPitch);
 #pragma unroll
                         for (int nt = 0; nt < D / 8; ++nt)
 #pragma unroll
                             for (int x = 0; x < 2; ++x) {
-                                const uint32_t bits = row[8 * nt + 2 * j + x];
+                                const uint32_t bits = reinterpret_cast<const uint16_t*>(vals + C::place(8 * i + t + u, nt))[2 * j + x];
                                 if ((bits & 0x7f80u) != 0x7f80u) continue;
                                 const float v = __uint_as_float(bits << 16);
                                 if (r0) acc.o[nt][x] += p0 * v;
@@ -262,139 +333,430 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                             }
                     }
                 }
-            team_barrier<WR>(WR == 1 ? 0 : (int)(threadIdx.x >> 5) / WR);
+            team_barrier<WR>(team);
             for (int x = lane; x < C::kTile * D; x += 32) {      // (every warp of the team writes the same zeros)
-                uint16_t* at = reinterpret_cast<uint16_t*>(vals + (x / D) * C::kPitch) + x % D;
+                uint16_t* at = reinterpret_cast<uint16_t*>(vals + C::place(x / D, x % D / 8)) + x % 8;
                 if ((*at & 0x7f80u) == 0x7f80u) *at = 0;
             }
-            team_barrier<WR>(WR == 1 ? 0 : (int)(threadIdx.x >> 5) / WR);
+            fence_async();
+            team_barrier<WR>(team);
         }
     }
-    // Weights go into the MMA as two bf16 pieces, the rounded weight and what the rounding left (2^-17 of it at most): one piece alone would
-    // add as much error as the rounding of the result, and at these rates the second MMA is free.
-    const uint32_t vrow = base + C::kHalf + (((lane >> 3) & 1) * 8 + (lane & 7)) * C::kPitch + (lane >> 4) * 16;
+    // bf16: weights go into the MMA as two pieces, the rounded weight and what the rounding left (2^-17 of it at most): one piece alone would
+    // add as much error as the rounding of the result, and at these rates the second MMA is free.  e4m3: one piece of f16 (2^-11).
+    const uint32_t v_row = ((lane >> 3) & 1) * 8 + (lane & 7), v_at = base + C::kHalf + v_row * C::kBox, v_vec = ((lane >> 4) ^ C::swizzle(v_row)) << 4;
 #pragma unroll
-    for (int g = 0; g < WR; ++g) {
+    for (int g = 0; g < C::kTile / 16; ++g) {
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                            // i: (row half, token half) of the A fragment
             const float x = s[2 * g + (i >> 1)][2 * (i & 1)], y = s[2 * g + (i >> 1)][2 * (i & 1) + 1];
-            hi[i] = pack_bf16(x, y);
-            lo[i] = pack_bf16(x - __uint_as_float(hi[i] << 16), y - __uint_as_float(hi[i] & 0xffff0000u));
+            if (F8) {
+                const __half2 h = __floats2half2_rn(x, y);
+                hi[i] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                hi[i] = pack_bf16(x, y);
+                lo[i] = pack_bf16(x - __uint_as_float(hi[i] << 16), y - __uint_as_float(hi[i] & 0xffff0000u));
+            }
         }
 #pragma unroll
         for (int c = 0; c < C::kRow / 32; ++c) {
             uint32_t b[4];
-            ldsm_t(b, vrow + g * 16 * C::kPitch + c * 32);
+            ldsm_t(b, v_at + (v_vec ^ (2 * c % kVecs << 4)) + 2 * c / kVecs * (C::kTile * C::kBox) + g * 16 * C::kBox);
             if (!F8) {
-                mma(acc.o[2 * c], hi, b[0], b[1]);
-                mma(acc.o[2 * c + 1], hi, b[2], b[3]);
-                mma(acc.o[2 * c], lo, b[0], b[1]);
-                mma(acc.o[2 * c + 1], lo, b[2], b[3]);
+                mma<false>(acc.o[2 * c], hi, b[0], b[1]);
+                mma<false>(acc.o[2 * c + 1], hi, b[2], b[3]);
+                mma<false>(acc.o[2 * c], lo, b[0], b[1]);
+                mma<false>(acc.o[2 * c + 1], lo, b[2], b[3]);
             } else {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {                    // 16 dims each
+                for (int x = 0; x < 2; ++x) {                    // 16 dims each: a word is (t0 d0, t0 d1, t1 d0, t1 d1)
                     uint32_t e0, o0, e1, o1;
-                    e4m3_pairs(b[2 * x], e0, o0);
-                    e4m3_pairs(b[2 * x + 1], e1, o1);
-                    mma(acc.o[4 * c + 2 * x], hi, e0, e1);
-                    mma(acc.o[4 * c + 2 * x + 1], hi, o0, o1);
-                    mma(acc.o[4 * c + 2 * x], lo, e0, e1);
-                    mma(acc.o[4 * c + 2 * x + 1], lo, o0, o1);
+                    e4m3_pairs<LIST>(__byte_perm(b[2 * x], 0, 0x3120), e0, o0);
+                    e4m3_pairs<LIST>(__byte_perm(b[2 * x + 1], 0, 0x3120), e1, o1);
+                    mma<true>(acc.o[4 * c + 2 * x], hi, e0, e1);
+                    mma<true>(acc.o[4 * c + 2 * x + 1], hi, o0, o1);
                 }
             }
         }
     }
 }
 
-// A warp's share of a unit's copy: 16 tokens, their keys and values.  Returns which of the tokens exist.
-struct AttSource {
-    const KvView* c;
-    int64_t seq, first;           // first: index of the list's entry 0 (tree) or 0
-    int len, head;
-    const uint16_t* list;         // LIST: node of each entry
-    Ctrl* ctrl;
+// The run of units of a CTA, segment by segment; the producer and the consumers walk it each on their own.
+struct AttWalk {
+    long long u, u1, off;         // next unit, end, and the next unit's place in its sequence
+    int seq;
+};
+struct AttSegment {
+    int seq, head, group, len, units, tile0, count;
+    int token, token_end;         // committed tokens of this segment
+    bool tree;                    // it holds the tree's tokens, too
 };
 
-template <int D, bool F8, int WR, bool LIST>
-__device__ __forceinline__ uint32_t att_load(const AttSource& src, uint8_t* stage, int group, int token0, int32_t page_id) {
-    using C = AttCfg<D, F8, WR>;
-    constexpr int V = C::kRow / 16;                              // 16-byte vectors of a row
-    const KvView& c = *src.c;
-    const int lane = threadIdx.x & 31;
-    const uint32_t dst = smem_addr(stage) + group * 16 * C::kPitch;
-    uint8_t* exps = stage + 2 * C::kHalf + group * 16;
-    const int n = min(max(src.len - token0, 0), 16);
-    if (!LIST && (c.page & 15) == 0) {                           // the 16 tokens lie in one page
-        const bool ok = (uint32_t)page_id < (uint32_t)c.n_pages;
-        const int have = ok ? n : 0;
-        if (!ok && n > 0 && lane == 0) kv_flag(src.ctrl);
-        const int in = token0 % c.page;
-        const int64_t at = ok ? (int64_t)page_id * c.stride_page + (int64_t)in * c.stride_token + src.head * c.stride_head : 0;
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const int x = i * 32 + lane, r = x / V, v = x % V;
-            const int64_t from = at + (r < have ? r * c.stride_token : 0) + v * 16;
-            cp16(dst + r * C::kPitch + v * 16, c.k + from, r < have);
-            cp16(dst + C::kHalf + r * C::kPitch + v * 16, c.v + from, r < have);
-        }
-        if (F8 && lane < 2) {
-            const int64_t e = ok ? ((int64_t)page_id * c.heads + src.head) * c.page + in : 0;
-            cp16(smem_addr(exps) + lane * C::kTile, (lane ? c.v_exp : c.k_exp) + e, have > 0);
-        }
-        return (1u << have) - 1u;
-    }
-    int64_t at = 0, e = 0;
-    bool ok = false;
-    if (lane < n) {
-        ok = kv_place(c, src.seq, src.first + (LIST ? (int64_t)src.list[token0 + lane] : (int64_t)(token0 + lane)), at, e);
-        if (!ok) kv_flag(src.ctrl);
-        at += src.head * c.stride_head;
-    }
-    if (F8 && lane < 16) {
-        e += (int64_t)src.head * c.page;
-        uint32_t a = 0, b = 0;
-        if (ok) {
-            asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(a) : "l"(c.k_exp + e) : "memory");
-            asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(b) : "l"(c.v_exp + e) : "memory");
-        }
-        exps[lane] = (uint8_t)a, exps[C::kTile + lane] = (uint8_t)b;
-    }
-    const uint32_t have = __ballot_sync(0xffffffffu, ok);
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-        const int x = i * 32 + lane, r = x / V, v = x % V;
-        const int64_t from = __shfl_sync(0xffffffffu, at, r) + v * 16;
-        cp16(dst + r * C::kPitch + v * 16, c.k + from, (have >> r) & 1);
-        cp16(dst + C::kHalf + r * C::kPitch + v * 16, c.v + from, (have >> r) & 1);
-    }
-    return have;
+__device__ __forceinline__ int att_len(const KvAttendArgs& a, int s) {
+    return (int)min((int64_t)max(ld_cg_s32(a.lens + s), 0), (int64_t)a.c.max_pages * a.c.page);
+}
+__device__ __forceinline__ int att_units(const KvAttendArgs& a, int len) {
+    return max((len + kAttUnit - 1) / kAttUnit + (a.node ? kAttTreeUnits : 0), 1);
+}
+__device__ __forceinline__ bool att_next(const KvAttendArgs& a, int groups, AttWalk& w, AttSegment& g) {
+    if (w.u >= w.u1) return false;
+    g.seq = w.seq;
+    g.len = att_len(a, g.seq);
+    g.units = att_units(a, g.len);
+    const int pair = (int)(w.off / g.units);
+    g.tile0 = (int)(w.off - (long long)pair * g.units);
+    g.count = (int)min((long long)(g.units - g.tile0), w.u1 - w.u);
+    g.head = pair / groups, g.group = pair - g.head * groups;
+    g.token = (int)min((long long)g.tile0 * kAttUnit, (long long)g.len);
+    g.token_end = (int)min((long long)(g.tile0 + g.count) * kAttUnit, (long long)g.len);
+    g.tree = a.node && g.tile0 + g.count == g.units;
+    w.u += g.count, w.off += g.count;
+    if (w.off == (long long)g.units * a.c.heads * groups) ++w.seq, w.off = 0;
+    return true;
 }
 
+// A producer's lane: a token of its tile.
+struct AttToken {
+    int32_t id, in;               // page (-1: out of range, -2: no token) and place in it
+    int head, flags;              // header of the tile
+    bool some;                    // the tile has tokens
+    bool have;                    // the round exists
+    unsigned long long mask;      // a tree's token: the rows that see it
+    uint32_t ke, ve;              // e4m3: its exponents' bytes
+};
+
 template <int D, bool F8, int WR>
-__global__ void __launch_bounds__(kAttThreads)
-k_kv_attend(const __grid_constant__ KvAttendArgs a) {
+struct AttProducer {
     using C = AttCfg<D, F8, WR>;
-    extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ float s_m[C::kTeams][16 * WR], s_l[C::kTeams][16 * WR];
-    __shared__ uint32_t s_seen[C::kStages][4];                   // of each stage, by warp: tokens that exist
-    __shared__ long long s_sum[4];
+    const KvAttendArgs& a;
+    const CUtensorMap *k_map, *v_map;
+    uint8_t *ring, *notes;        // of this producer
+    uint64_t *full, *empty;
+    int16_t* parents;
+    volatile int* dead;
+    AttWalk walk;
+    AttSegment g;
+    int groups, lane, feed;
+    int mode;                     // 0: the next segment, 1: committed tokens, 2: the tree's, 3: a round of none
+    bool told;                    // the round before has told its teams that it was their last
+    int tree_of, n0, n1, f0, f1;  // whose parents are here; nodes of rows lane and lane + 32, and where they have got to
+    int place = 0, filled = 0;    // of the next tile, in the ring; tiles so far
+    uint32_t parity = 1;          // (an empty ring's places count as given back)
+
+    // This lane's token of the next round: its place in the sequence; false: no more rounds.  Every team is told which tile of a segment is its
+    // last; with more teams than producers the last two rounds are, if need be one of no tokens.
+    __device__ bool token(int32_t& index, AttToken& r, int& seq) {
+        if (mode == 0) {
+            if (!att_next(a, groups, walk, g)) return false;
+            mode = g.token >= g.token_end && g.tree ? 2 : 1;
+            told = false;
+            if (g.tree) load_tree();
+        }
+        seq = g.seq, r.head = g.head;
+        r.flags = 0, r.mask = 0, index = -1;
+        bool last = mode == 3, before_last = false;
+        int n = 0;                                               // tokens of the round
+        if (mode == 1) {
+            n = min(g.token_end - g.token, kAttRound);
+            const int t = kAttTile * feed + lane;
+            if (t < n) index = g.token + t;
+            g.token += n;
+            last = g.token >= g.token_end && !g.tree;
+            before_last = g.token < g.token_end && g.token + kAttRound >= g.token_end && !g.tree;
+            if (g.token >= g.token_end && g.tree) mode = 2;
+        } else if (mode == 2) {
+            // the nodes that some row sees, largest first: the rows' walks to the root are merged (by every producer, for its own tokens)
+            r.flags = kAttTree;
+            for (; n < kAttRound; ++n) {
+                const int f = __reduce_max_sync(0xffffffffu, max(f0, f1));
+                if (f < 0) break;
+                const unsigned lo = __ballot_sync(0xffffffffu, f0 == f), hi = __ballot_sync(0xffffffffu, f1 == f);
+                if (n == kAttTile * feed + lane) index = (int32_t)min((int64_t)g.len + f, (int64_t)INT32_MAX), r.mask = ((unsigned long long)hi << 32) | lo;
+                const int up = a.parent ? (int)parents[f] : f - 1;
+                f0 = f0 == f ? up : f0, f1 = f1 == f ? up : f1;
+            }
+            last = __reduce_max_sync(0xffffffffu, max(f0, f1)) < 0;
+        }
+        r.some = kAttTile * feed < n;
+        if (last) mode = mode == 3 || told || C::kShare == 1 ? 0 : 3;
+        told = before_last && C::kShare > 1;
+        // (of two tiles of a round the second is the team's last)
+        if ((last && (WR < 4 || feed >= 2)) || told) r.flags |= kAttEnd;
+        return true;
+    }
+
+    __device__ void load_tree() {
+        if (tree_of != g.seq) {
+            tree_of = g.seq;
+            const int N = a.N;
+            if (a.parent) {
+                feeds_barrier();                                 // (the others have done with the parents before)
+                for (int i = 32 * feed + lane; i < N; i += 32 * kAttFeeds) {               // (a parent that does not lie in front ends the walk)
+                    const int p = ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i);
+                    parents[i] = (int16_t)(p >= 0 && p < i ? p : -1);
+                }
+            }
+            auto node = [&](int row) {
+                const int f = row < a.Q ? ld_cg_s32(a.node + (int64_t)g.seq * a.Q + row) : -1;
+                if (f >= N) kv_flag(a.ctrl);
+                return f < 0 || f >= N ? -1 : f;
+            };
+            n0 = node(lane), n1 = node(lane + 32);
+            if (a.parent) feeds_barrier();
+        }
+        f0 = n0, f1 = n1;
+    }
+
+    // a lane's token -> its page id (the load is left in flight)
+    __device__ void look_up(AttToken& p) {
+        int32_t index;
+        int seq = 0;
+        p.have = token(index, p, seq);
+        p.id = -2, p.in = 0;
+        if (!p.have || index < 0) return;
+        const uint32_t page = a.page_shift >= 0 ? (uint32_t)index >> a.page_shift : (uint32_t)index / (uint32_t)a.c.page;
+        p.in = index - (int32_t)(page * (uint32_t)a.c.page);
+        p.id = page < (uint32_t)a.c.max_pages ? ld_cg_s32(a.c.pages + (int64_t)seq * a.c.pages_ld + page) : -1;
+    }
+    // page id -> exponents (left in flight, too)
+    __device__ void resolve(AttToken& p) {
+        if (p.id != -2 && (uint32_t)p.id >= (uint32_t)a.c.n_pages) {
+            kv_flag(a.ctrl);
+            p.id = -2;
+        }
+        p.ke = p.ve = 0;
+        if (F8 && p.id >= 0) {
+            const int64_t e = ((int64_t)p.id * a.c.heads + p.head) * a.c.page + p.in;
+            asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(p.ke) : "l"(a.c.k_exp + e) : "memory");
+            asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(p.ve) : "l"(a.c.v_exp + e) : "memory");
+        }
+    }
+
+    __device__ void emit(const AttToken& r) {
+        uint8_t *tile = ring + place * C::kSlot, *note = notes + place * C::kNote;
+        att_wait(empty + place, parity, dead, a.ctrl);
+        if (r.some) {
+            const bool ok = r.id >= 0;
+            const unsigned have = __ballot_sync(0xffffffffu, ok);
+            // 16 or 32 tokens of a page at a time by tensor copies, where they are all there
+            unsigned boxed = 0;                                  // tokens that come so
+            if (a.box == 32 && have == 0xffffffffu && !(r.flags & kAttTree)) boxed = have;
+            else if (a.box == 16 && !(r.flags & kAttTree)) boxed = ((have & 0xffffu) == 0xffffu ? 0xffffu : 0u) | ((have >> 16) == 0xffffu ? 0xffff0000u : 0u);
+            if (boxed) {
+                const int id0 = __shfl_sync(0xffffffffu, r.id, 0), in0 = __shfl_sync(0xffffffffu, r.in, 0);
+                const int id1 = __shfl_sync(0xffffffffu, r.id, 16), in1 = __shfl_sync(0xffffffffu, r.in, 16);
+                if (elect_lane()) {
+                    uint64_t* bar = full + place;
+                    mbar_expect(bar, __popc(boxed) * 2 * C::kRow);
+                    const uint32_t dst = smem_u32(tile);
+#pragma unroll
+                    for (int x = 0; x < C::kRow / C::kBox; ++x) {
+                        const uint32_t to = dst + x * C::kTile * C::kBox;
+                        const int dim = x * (F8 ? C::kBox : C::kBox / 2);
+                        if (boxed & 1u) {
+                            box_copy(to, k_map, dim, in0, r.head, id0, bar);
+                            box_copy(to + C::kHalf, v_map, dim, in0, r.head, id0, bar);
+                        }
+                        if (a.box == 16 && (boxed >> 31)) {
+                            box_copy(to + 16 * C::kBox, k_map, dim, in1, r.head, id1, bar);
+                            box_copy(to + C::kHalf + 16 * C::kBox, v_map, dim, in1, r.head, id1, bar);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+            if (boxed != 0xffffffffu) {
+                // the others through registers, missing rows as zeros (a weight of zero does not undo what lay there)
+                constexpr int V = C::kRow / 16, kAhead = V % 4 == 0 ? 4 : 3;               // vectors of a row; of keys and of values in flight
+                const int64_t mine = ok ? (int64_t)r.id * a.c.stride_page + (int64_t)r.in * a.c.stride_token + r.head * a.c.stride_head : -1;
+                for (int x0 = 0; x0 < kAttTile * V; x0 += 32 * kAhead) {
+                    uint4 kx[kAhead], vx[kAhead];
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int x = x0 + 32 * u + lane, line = x / V, v = x - line * V;
+                        const int64_t at = __shfl_sync(0xffffffffu, mine, line);
+                        kx[u] = vx[u] = make_uint4(0, 0, 0, 0);
+                        if (at >= 0 && !(boxed >> line & 1)) kx[u] = ld_once_u4(a.c.k + at + v * 16), vx[u] = ld_once_u4(a.c.v + at + v * 16);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int x = x0 + 32 * u + lane, line = x / V, v = x - line * V;
+                        if (boxed >> line & 1) continue;
+                        uint8_t* to = tile + C::place(line, v);
+                        *reinterpret_cast<uint4*>(to) = kx[u];
+                        *reinterpret_cast<uint4*>(to + C::kHalf) = vx[u];
+                    }
+                }
+                fence_async();                                   // (the place's next tile may come by tensor copies)
+            }
+            if (F8)
+                *reinterpret_cast<float4*>(note + 16 * lane) =
+                    make_float4(kv_two_to(r.ke), ok ? 0.0f : -INFINITY, (float)min(max((int)r.ve - 127, -100), 112), ok ? kv_two_to(r.ve) : 0.0f);
+            else
+                *reinterpret_cast<float*>(note + 4 * lane) = ok ? 0.0f : -INFINITY;
+            if (r.flags & kAttTree) *reinterpret_cast<unsigned long long*>(note + C::kMasks + 8 * lane) = r.mask;
+        }
+        if (lane == 0) *reinterpret_cast<volatile uint32_t*>(note + C::kHeader) = (uint32_t)r.flags | (r.some ? 0u : (uint32_t)kAttEmpty);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full + place);
+        ++filled;
+        if (++place == C::kPer) place = 0, parity ^= 1;
+    }
+
+    __device__ void run() {
+        AttToken now, next, later;                               // exponents are asked for a round, page ids two rounds ahead of the copies
+        look_up(now);
+        resolve(now);
+        next.have = false;
+        if (now.have) look_up(next);
+        while (now.have) {
+            if (next.have) resolve(next);
+            later.have = false;
+            if (next.have) look_up(later);
+            emit(now);
+            now = next;
+            next = later;
+        }
+        // No copy is in flight when the CTA ends, also when a wait has run out: the last use of every place in the ring lands.
+        for (int k = max(0, filled - C::kPer); k < filled; ++k) {
+            const unsigned long long t0 = global_ns();
+            while (!mbar_try(full + k % C::kPer, k / C::kPer & 1) && global_ns() - t0 < kAttWaitNs) {}
+        }
+    }
+};
+
+// A query row into fragments' registers or (heads over 128) shared memory: in two steps, so that the next segment's rows are on their way while
+// this one's results meet.
+template <int D, bool F8, int WR>
+struct AttQueries {
+    using C = AttCfg<D, F8, WR>;
+    static constexpr int kWords = (D / 4 + 31) / 32;             // in shared memory: a warp a row, a lane has kWords times four dims
+    static constexpr int kLines = (16 * WR + kAttWarps - 1) / kAttWarps;
+    uint32_t f[C::kQRegs ? D / 16 : 1][4];
+    uint2 w[C::kQRegs ? 1 : kLines][kWords];
+
+    __device__ __forceinline__ static const uint16_t* row_of(const KvAttendArgs& a, const AttSegment& g, int row) {
+        const int rows = a.Q * a.group, r = min(row, rows - 1), qi = r / a.group;
+        return a.q + ((int64_t)g.seq * a.Q + qi) * a.q_ld + (int64_t)(g.head * a.group + (r - qi * a.group)) * D;
+    }
+    __device__ __forceinline__ void fetch(const KvAttendArgs& a, const AttSegment& g, int warp, int lane) {
+        const int rows = a.Q * a.group, row0 = g.group * 16 * WR, j = lane & 3;
+        if (C::kQRegs) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = row0 + warp % WR * 16 + (lane >> 2) + 8 * r;
+                const uint16_t* q = row_of(a, g, row);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    if (!F8) {
+                        f[ks][r] = row < rows ? ld_cg_u32(reinterpret_cast<const uint32_t*>(q + 16 * ks + 2 * j)) : 0u;
+                        f[ks][2 + r] = row < rows ? ld_cg_u32(reinterpret_cast<const uint32_t*>(q + 16 * ks + 8 + 2 * j)) : 0u;
+                    } else {                                     // dims in the order in which a word of the keys holds them
+                        const uint2 x = row < rows ? ld_cg_u2(reinterpret_cast<const uint2*>(q + 16 * ks + 4 * j)) : make_uint2(0, 0);
+                        f[ks][r] = x.x, f[ks][2 + r] = x.y;
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kLines; ++k) {
+                const int row = row0 + warp + k * kAttWarps;
+                const uint16_t* q = row_of(a, g, row);
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) {
+                    const int c = i * 32 + lane;
+                    w[k][i] = row < rows && c < D / 4 ? ld_cg_u2(reinterpret_cast<const uint2*>(q + 4 * c)) : make_uint2(0, 0);
+                }
+            }
+        }
+    }
+    // ... and the factors of the warp's rows' scores
+    __device__ __forceinline__ void settle(float scale_log2, float (&scale)[2], uint8_t* qs, float* s_qscale, int warp, int lane) {
+        scale[0] = scale[1] = scale_log2;
+        if constexpr (C::kQRegs) {
+            if (!F8) return;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int x = r; x < 4; x += 2) top = max(top, max(f[ks][x] << 16 & 0x7fff0000u, f[ks][x] & 0x7fff0000u));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const int power = q_power(top);
+                const float k = two_to(power);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int x = r; x < 4; x += 2) f[ks][x] = q_pair(f[ks][x], k);
+                scale[r] *= two_to(-power);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kLines; ++k) {
+                const int r = warp + k * kAttWarps;
+                if (r >= 16 * WR) break;
+                float p = 1.0f;
+                if (F8) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i)
+                        top = max(max(top, max(w[k][i].x << 16 & 0x7fff0000u, w[k][i].x & 0x7fff0000u)), max(w[k][i].y << 16 & 0x7fff0000u, w[k][i].y & 0x7fff0000u));
+                    top = __reduce_max_sync(0xffffffffu, top);
+                    p = two_to(q_power(top));
+                    if (lane == 0) s_qscale[r] = two_to(-q_power(top));
+                }
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) {
+                    const int c = i * 32 + lane;
+                    if (c >= D / 4) continue;
+                    if (!F8) *reinterpret_cast<uint2*>(qs + r * C::kQPitch + c * 8) = w[k][i];
+                    else {                                           // dims 4 j .. 4 j + 3 of 16 go to columns 2 j, 2 j + 1 and 8 + 2 j, 9 + 2 j
+                        uint8_t* to = qs + r * C::kQPitch + (c >> 2) * 32 + (c & 3) * 4;
+                        *reinterpret_cast<uint32_t*>(to) = q_pair(w[k][i].x, p);
+                        *reinterpret_cast<uint32_t*>(to + 16) = q_pair(w[k][i].y, p);
+                    }
+                }
+            }
+            consumers_barrier();
+            if (F8) scale[0] *= s_qscale[warp % WR * 16 + (lane >> 2)], scale[1] *= s_qscale[warp % WR * 16 + (lane >> 2) + 8];
+        }
+    }
+};
+
+template <int D, bool F8, int WR>
+__global__ void __launch_bounds__(kAttThreads, 1)
+k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using C = AttCfg<D, F8, WR>;
+    extern __shared__ uint8_t raw[];                             // the ring, its tiles' notes, queries, meeting place, parents
+    uint8_t* ring = raw + (-smem_u32(raw) & 1023u);
+    __shared__ uint64_t s_full[C::kSlots], s_empty[C::kSlots];
+    __shared__ float s_qscale[C::kQRegs ? 1 : 16 * WR];          // powers that the queries' rows were scaled by, undone in the scores
+    __shared__ long long s_sum[kAttWarps + kAttFeeds];
     __shared__ long long s_at;
-    __shared__ int s_seq, s_warp_count[4];
+    __shared__ int s_seq, s_dead;
+    uint8_t* notes = ring + C::kSlots * C::kSlot;
+    uint8_t* qs = notes + C::kSlots * C::kNote;
+    float4* meet = reinterpret_cast<float4*>(qs + C::kQBytes);
+    int16_t* parents = reinterpret_cast<int16_t*>(qs + C::kQBytes + C::kMeet);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid < C::kSlots) {
+        mbar_init(s_full + tid, 1);                              // the producer's word that all but its copies is there
+        mbar_init(s_empty + tid, WR);
+    }
+    if (tid == 0) s_dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     griddep_launch_dependents();
     griddep_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, team = warp / WR, wr = warp % WR, j = lane & 3;
     const int rows = a.Q * a.group, groups = (rows + 16 * WR - 1) / (16 * WR);
-    const int64_t per_tile = (int64_t)a.c.heads * groups;
-    const int64_t room = (int64_t)a.c.max_pages * a.c.page;
-    const bool tree = a.node != nullptr;
-    auto len_of = [&](int s) { return (int)min((int64_t)max(ld_cg_s32(a.lens + s), 0), room); };
-    auto units_of = [&](int s) { return max((len_of(s) + C::kTile - 1) / C::kTile + (tree ? 1 : 0), 1); };
+    const int64_t per_unit = (int64_t)a.c.heads * groups;
 
     // this CTA's run of units: [u0, u1) of all sequences' units laid end to end
     const int chunk = (a.c.S + kAttThreads - 1) / kAttThreads, sa = min(tid * chunk, a.c.S), sb = min(sa + chunk, a.c.S);
     long long mine = 0;
-    for (int s = sa; s < sb; ++s) mine += units_of(s);
+    for (int s = sa; s < sb; ++s) mine += att_units(a, att_len(a, s));
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -404,276 +766,232 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a) {
     if (lane == 31) s_sum[warp] = incl;
     __syncthreads();
     long long before = incl - mine, total = 0;
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < kAttWarps + kAttFeeds; ++w) {
         if (w < warp) before += s_sum[w];
         total += s_sum[w];
     }
-    total *= per_tile;
-    before *= per_tile;
-    mine *= per_tile;
-    // a CTA gets a unit for each team at the least
-    const long long ctas = min((long long)gridDim.x, max((total + C::kTeams - 1) / C::kTeams, 1ll));
-    const long long u0 = min(total * blockIdx.x / ctas, total), u1 = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : u0;
-    if (tid == 0 && (blockIdx.x >= ctas || u0 == u1)) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    if (blockIdx.x >= ctas || u0 == u1) return;
-    if (u0 >= before && u0 < before + mine) {                    // one thread's sequences hold the first unit
+    total *= per_unit;
+    before *= per_unit;
+    mine *= per_unit;
+    const long long ctas = min((long long)gridDim.x, total);
+    const bool idle = blockIdx.x >= ctas;
+    if (idle) {
+        if (tid == 0) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        return;
+    }
+    AttWalk walk;
+    walk.u = total * blockIdx.x / ctas;
+    walk.u1 = total * (blockIdx.x + 1) / ctas;
+    if (walk.u >= before && walk.u < before + mine) {            // one thread's sequences hold the first unit
         long long at = before;
         int s = sa;
-        while (s < sb - 1 && at + units_of(s) * per_tile <= u0) at += units_of(s++) * per_tile;
+        while (s < sb - 1) {
+            const long long n = att_units(a, att_len(a, s)) * per_unit;
+            if (at + n > walk.u) break;
+            at += n;
+            ++s;
+        }
         s_seq = s;
-        s_at = u0 - at;
+        s_at = walk.u - at;
     }
     __syncthreads();
-    int seq = s_seq;
-    long long off = s_at, u = u0;
+    walk.seq = s_seq;
+    walk.off = s_at;
+
+    if (warp >= kAttWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAttProducerRegs));
+        const int feed = warp - kAttWarps;
+        AttProducer<D, F8, WR> p{a, &k_map, &v_map, ring + feed * C::kPer * C::kSlot, notes + feed * C::kPer * C::kNote, s_full + feed * C::kPer,
+                                 s_empty + feed * C::kPer, parents, &s_dead, walk, {}, groups, lane, feed, 0, false, -1, -1, -1, -1, -1};
+        p.run();
+        return;
+    }
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kAttConsumerRegs));
+
+    const int team = warp / WR, wr = warp % WR, j = lane & 3;
     int4 meta = make_int4(-1, 0, 0, 0);
-
-    while (u < u1) {
-        const int len = len_of(seq), units = units_of(seq);
-        const int pair = (int)(off / units), tile0 = (int)(off - (long long)pair * units);
-        const int count = (int)min((long long)(units - tile0), u1 - u);
-        const int head = pair / groups, group = pair - head * groups;
-        const int full = (len + C::kTile - 1) / C::kTile;        // units of committed tokens
-        const int t1 = min(tile0 + count, full);
-        const bool with_tree = tree && tile0 + count == units;
-        const int row0 = group * 16 * WR, n_rows = min(rows - row0, 16 * WR);
-        AttSource src{&a.c, seq, 0, len, head, nullptr, a.ctrl};
-
-        // the ring's first units, then (while they come) the queries
-        int issue = tile0 + team;
-        auto page_of = [&](int tile) {
-            const int token = tile * C::kTile + 16 * wr;
-            return tile < t1 && token < len ? ld_cg_s32(a.c.pages + (int64_t)seq * a.c.pages_ld + (uint32_t)token / (uint32_t)a.c.page) : -1;
-        };
-        int32_t page_id = page_of(issue);
-        auto fill = [&](int slot) {
-            if (issue < t1) {
-                const int32_t id = page_id;
-                page_id = page_of(issue + C::kTeams);
-                const uint32_t have = att_load<D, F8, WR, false>(src, ring + slot * C::kCtaStage + team * C::kStage, wr, issue * C::kTile + 16 * wr, id);
-                if (lane == 0) s_seen[slot][warp] = have;
-            }
-            issue += C::kTeams;
-            cp_commit();
-        };
-#pragma unroll
-        for (int i = 0; i < C::kStages - 1; ++i) fill(i);
-
-        uint32_t qf[C::kQRegs ? D / 16 : 1][4];
+    // the team's next tile: its producer, and its place there.  Eight teams: two to a producer, in turn; two: two producers each, in turn.
+    int feed = team % kAttFeeds, place = team / kAttFeeds;
+    uint32_t parity = 0;
+    AttSegment g, after;
+    AttQueries<D, F8, WR> q;
+    long long at = walk.u;
+    att_next(a, groups, walk, g);
+    q.fetch(a, g, warp, lane);
+    for (bool go_on = true; go_on; g = after) {
+        const int row0 = g.group * 16 * WR;
         const int r0 = row0 + wr * 16 + (lane >> 2), r1 = r0 + 8;
         const int qi0 = min(r0, rows - 1) / a.group, qi1 = min(r1, rows - 1) / a.group;
-        if (C::kQRegs) {
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int row = r ? r1 : r0, qi = r ? qi1 : qi0;
-                const uint16_t* q = a.q + ((int64_t)seq * a.Q + qi) * a.q_ld + (int64_t)(head * a.group + (min(row, rows - 1) - qi * a.group)) * D;
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    if (!F8) {
-                        qf[ks][r] = row < rows ? ld_cg_u32(reinterpret_cast<const uint32_t*>(q + 16 * ks + 2 * j)) : 0u;
-                        qf[ks][2 + r] = row < rows ? ld_cg_u32(reinterpret_cast<const uint32_t*>(q + 16 * ks + 8 + 2 * j)) : 0u;
-                    } else {                                     // dims in the order in which e4m3_pairs gives the keys'
-                        const uint2 w = row < rows ? ld_cg_u2(reinterpret_cast<const uint2*>(q + 16 * ks + 4 * j)) : make_uint2(0, 0);
-                        qf[ks][r] = __byte_perm(w.x, w.y, 0x5410);
-                        qf[ks][2 + r] = __byte_perm(w.x, w.y, 0x7632);
-                    }
-                }
-            }
-        } else {
-            uint8_t* qs = ring + C::kRing;
-            for (int x = tid; x < 16 * WR * (D / 4); x += kAttThreads) {
-                const int r = x / (D / 4), c = x % (D / 4), row = row0 + r, qi = min(row, rows - 1) / a.group;
-                const uint2 w = row < rows ? ld_cg_u2(reinterpret_cast<const uint2*>(a.q + ((int64_t)seq * a.Q + qi) * a.q_ld +
-                                                                                       (int64_t)(head * a.group + (row - qi * a.group)) * D + 4 * c))
-                                           : make_uint2(0, 0);
-                if (!F8) *reinterpret_cast<uint2*>(qs + r * C::kQPitch + c * 8) = w;
-                else {                                           // dims 4 j .. 4 j + 3 of 16 go to columns 2 j, 2 j + 1 and 8 + 2 j, 9 + 2 j (even, odd)
-                    uint8_t* at = qs + r * C::kQPitch + (c >> 2) * 32 + (c & 3) * 4;
-                    *reinterpret_cast<uint32_t*>(at) = __byte_perm(w.x, w.y, 0x5410);
-                    *reinterpret_cast<uint32_t*>(at + 16) = __byte_perm(w.x, w.y, 0x7632);
-                }
-            }
-            __syncthreads();
-        }
-        const uint32_t q_smem = smem_addr(ring + C::kRing) + wr * 16 * C::kQPitch;
+        float scale[2];
+        q.settle(a.scale_log2, scale, qs, s_qscale, warp, lane);
+        const uint32_t q_smem = smem_u32(qs) + wr * 16 * C::kQPitch;
 
         AttAcc<D> acc;
         acc.clear();
-        int slot = 0;
-        for (int t = tile0 + team; t < t1; t += C::kTeams) {
-            cp_wait<C::kStages - 2>();
-            team_barrier<WR>(team);
-            fill(slot == 0 ? C::kStages - 1 : slot - 1);
-            uint64_t seen = 0;
-#pragma unroll
-            for (int w = 0; w < WR; ++w) seen |= (uint64_t)s_seen[slot][team * WR + w] << (16 * w);
-            att_tile<D, F8, WR, false>(acc, qf, q_smem, ring + slot * C::kCtaStage + team * C::kStage, seen, a.scale_log2, nullptr, 0, 0);
-            slot = slot + 1 == C::kStages ? 0 : slot + 1;
-        }
-        cp_wait<0>();
-        __syncthreads();
-
-        if (with_tree) {
-            // which of the tree's nodes some row sees, and which rows see each: rows walk from their node to the root
-            uint8_t* room_at = ring + C::kCtaStage;
-            unsigned long long* mask = reinterpret_cast<unsigned long long*>(room_at);
-            int* parent = reinterpret_cast<int*>(room_at + 8 * kKvMaxNodes);
-            uint16_t* list = reinterpret_cast<uint16_t*>(room_at + 12 * kKvMaxNodes);
-            const int N = a.N;
-            for (int i = tid; i < N; i += kAttThreads) {
-                mask[i] = 0;
-                parent[i] = a.parent ? ld_cg_s32(a.parent + (int64_t)seq * a.parent_ld + i) : i - 1;
+        for (bool more = true; more;) {
+            const int slot = feed * C::kPer + place;
+            att_wait(s_full + slot, parity, &s_dead, a.ctrl);
+            uint8_t* tile = ring + slot * C::kSlot;
+            const uint8_t* note = notes + slot * C::kNote;
+            const uint32_t header = *reinterpret_cast<const volatile uint32_t*>(note + C::kHeader);
+            if (!(header & kAttEmpty)) {
+                if (header & kAttTree) att_tile<D, F8, WR, true>(acc, q.f, q_smem, tile, note, scale, qi0, qi1);
+                else att_tile<D, F8, WR, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
             }
-            __syncthreads();
-            if (tid < a.Q) {
-                int f = ld_cg_s32(a.node + (int64_t)seq * a.Q + tid);
-                if (f >= N) {
-                    kv_flag(a.ctrl);
-                    f = -1;
-                }
-                while (f >= 0) {                                 // (a parent lies in front of its child, so this ends)
-                    atomicOr(&mask[f], 1ull << tid);
-                    const int up = parent[f];
-                    f = up < f ? up : -1;
-                }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(s_empty + slot);
+            if (WR == 4) feed ^= 2;
+            if (WR < 4 || feed < 2) {
+                place += C::kShare;
+                if (place >= C::kPer) place -= C::kPer, parity ^= 1;
             }
-            __syncthreads();
-            int kept = 0;
-            for (int i0 = 0; i0 < N; i0 += kAttThreads) {
-                const int i = i0 + tid;
-                const unsigned long long bits = i < N ? mask[i] : 0;
-                const unsigned b = __ballot_sync(0xffffffffu, bits != 0);
-                if (lane == 0) s_warp_count[warp] = __popc(b);
-                __syncthreads();                                 // (the 128 masks have been read: the list's end is at or before them)
-                int at = kept + __popc(b & lanemask_lt());
-                for (int w = 0; w < 4; ++w) {
-                    if (w < warp) at += s_warp_count[w];
-                    kept += s_warp_count[w];
-                }
-                if (bits) mask[at] = bits, list[at] = (uint16_t)i;
-                __syncthreads();
-            }
-            AttSource nodes{&a.c, seq, len, kept, head, list, a.ctrl};
-            for (int t = team; t * C::kTile < kept; t += C::kTeams) {
-                uint8_t* stage = ring + team * C::kStage;
-                team_barrier<WR>(team);                          // (the tile before has been used)
-                const uint32_t have = att_load<D, F8, WR, true>(nodes, stage, wr, t * C::kTile + 16 * wr, 0);
-                if (lane == 0) s_seen[0][warp] = have;
-                cp_commit();
-                cp_wait<0>();
-                team_barrier<WR>(team);
-                uint64_t seen = 0;
-#pragma unroll
-                for (int w = 0; w < WR; ++w) seen |= (uint64_t)s_seen[0][team * WR + w] << (16 * w);
-                att_tile<D, F8, WR, true>(acc, qf, q_smem, stage, seen, a.scale_log2, mask + t * C::kTile, qi0, qi1);
-            }
-            __syncthreads();
+            more = !(header & kAttEnd) && !*const_cast<volatile int*>(&s_dead);
         }
 
-        // the teams' parts meet in shared memory
+        const long long at_next = walk.u;
+        go_on = att_next(a, groups, walk, after);
+        if (go_on) q.fetch(a, after, warp, lane);                // (on their way while the results meet)
+        if (WR == 4) feed = team;
+
+        // the teams' parts meet, the upper half's with the lower half's: a lane hands its share to the lane with the same rows and dims
+        consumers_barrier();                                     // (the meeting place is free)
+        constexpr int kShare = D / 8 + 1;                        // vectors of a lane
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            acc.l[r] += __shfl_xor_sync(0xffffffffu, acc.l[r], 1);
-            acc.l[r] += __shfl_xor_sync(0xffffffffu, acc.l[r], 2);
-            if (j == 0) {
-                s_m[team][wr * 16 + (lane >> 2) + 8 * r] = acc.m[r];
-                s_l[team][wr * 16 + (lane >> 2) + 8 * r] = acc.l[r];
+        for (int half = C::kTeams / 2; half >= 1; half /= 2) {
+            // who gives uses the place that it has read from: its own place, or in the first step that of the reader
+            float4* place = meet + (team >= half && half == C::kTeams / 2 ? warp - half * WR : warp) * kShare * 32 + lane;
+            if (team >= half && team < 2 * half) {
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) place[32 * i] = make_float4(acc.o[i][0], acc.o[i][1], acc.o[i][2], acc.o[i][3]);
+                place[32 * (D / 8)] = make_float4(acc.m[0], acc.m[1], acc.l[0], acc.l[1]);
             }
-        }
-        __syncthreads();
-        float* obuf = reinterpret_cast<float*>(ring);
+            consumers_barrier();
+            if (team < half) {
+                const float4* from = half == C::kTeams / 2 ? place : place + half * WR * kShare * 32;
+                const float4 y = from[32 * (D / 8)];
+                const float ym[2] = {y.x, y.y}, yl[2] = {y.z, y.w};
+                float fa[2], fb[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int lr = wr * 16 + (lane >> 2) + 8 * r;
-            float m = s_m[0][lr];
-#pragma unroll
-            for (int w = 1; w < C::kTeams; ++w) m = fmaxf(m, s_m[w][lr]);
-            const float f = acc.m[r] == -INFINITY ? 0.0f : exp2_fast(acc.m[r] - m);
-            if (lr < n_rows) {
-                float* o = obuf + (team * 16 * WR + lr) * C::kOPitch;
+                for (int r = 0; r < 2; ++r) {
+                    const float m = fmaxf(acc.m[r], ym[r]);
+                    fa[r] = acc.m[r] == -INFINITY ? 1.0f : exp2_fast(acc.m[r] - m);   // (a part of no token: nothing to scale)
+                    fb[r] = ym[r] == -INFINITY ? 1.0f : exp2_fast(ym[r] - m);
+                    acc.m[r] = m;
+                    acc.l[r] = acc.l[r] * fa[r] + yl[r] * fb[r];
+                }
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) {
-                    const int d0 = o_dim<F8>(i, j);
-                    const bool none = acc.m[r] == -INFINITY && acc.l[r] == 0.0f;
-                    o[d0] = none ? 0.0f : acc.o[i][2 * r] * f;
-                    o[d0 + (F8 ? 2 : 1)] = none ? 0.0f : acc.o[i][2 * r + 1] * f;
+                    const float4 x = from[32 * i];
+                    acc.o[i][0] = acc.o[i][0] * fa[0] + x.x * fb[0], acc.o[i][1] = acc.o[i][1] * fa[0] + x.y * fb[0];
+                    acc.o[i][2] = acc.o[i][2] * fa[1] + x.z * fb[1], acc.o[i][3] = acc.o[i][3] * fa[1] + x.w * fb[1];
                 }
             }
         }
-        __syncthreads();
-        const bool whole = count == units;
-        const int slot_of = 2 * blockIdx.x + (tile0 == 0 ? 1 : 0);
-        float* part = a.part + (int64_t)slot_of * a.part_rows * (D + 2);
-        for (int x = tid; x < n_rows * (D / 4); x += kAttThreads) {
-            const int lr = x / (D / 4), c = x % (D / 4);
-            float m = s_m[0][lr], l = 0.0f;
+        const bool whole = g.count == g.units;
+        if (!whole && g.tile0 == 0)                              // the last CTA with units of this (sequence, head, group)
+            meta = make_int4((int)(((at + g.units) * ctas - 1) / total), g.seq, g.head, g.group);
+        at = at_next;
+        if (team != 0) continue;
+        const bool broken = *const_cast<volatile int*>(&s_dead) != 0;
+        float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * (D + 2);
 #pragma unroll
-            for (int w = 1; w < C::kTeams; ++w) m = fmaxf(m, s_m[w][lr]);
-            float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll
-            for (int w = 0; w < C::kTeams; ++w) {
-                const float lw = s_l[w][lr];
-                l += s_m[w][lr] == -INFINITY ? lw : lw * exp2_fast(s_m[w][lr] - m);
-                const float4 y = *reinterpret_cast<const float4*>(obuf + (w * 16 * WR + lr) * C::kOPitch + 4 * c);
-                o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
-            }
-            const int row = row0 + lr, qi = row / a.group;
-            const int64_t t = (int64_t)seq * a.Q + qi;
-            const int64_t at = t * a.Hq + head * a.group + (row - qi * a.group);
-            if (tree && ld_cg_s32(a.node + t) < -1) {            // a row of no token
-                m = -INFINITY, l = 0.0f;
-                o = make_float4(0, 0, 0, 0);
-            }
+        for (int r = 0; r < 2; ++r) {
+            float l = acc.l[r];
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
+            float m = acc.m[r];
+            const int row = r ? r1 : r0, qi = r ? qi1 : qi0;
+            if (row >= rows) continue;
+            const int64_t t = (int64_t)g.seq * a.Q + qi, to = t * a.Hq + g.head * a.group + (row - qi * a.group);
+            const bool blind = a.node && ld_cg_s32(a.node + t) < -1;                       // a row of no token
+            if (broken) l = NAN;
+            const bool none = blind || l == 0.0f;
+            if (blind) m = -INFINITY, l = 0.0f;
+            const float inv = whole ? 1.0f / l : 1.0f;
+            const int lr = row - row0;
             if (whole) {
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                const bool none = l == 0.0f;
-                *reinterpret_cast<uint2*>(a.out + at * D + 4 * c) =
-                    none ? make_uint2(0, 0) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-                if (c == 0 && a.lse) a.lse[at] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-            } else {
-                *reinterpret_cast<float4*>(part + lr * D + 4 * c) = o;
-                if (c == 0) part[a.part_rows * D + lr] = m, part[a.part_rows * (D + 1) + lr] = l;
+                if (j == 0 && a.lse) a.lse[to] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            } else if (j == 0) {
+                part[a.part_rows * D + lr] = m, part[a.part_rows * (D + 1) + lr] = l;
+            }
+#pragma unroll
+            for (int i = 0; i < D / 8; i += F8 ? 2 : 1) {
+                float x[4];
+                if (F8) x[0] = acc.o[i][2 * r], x[1] = acc.o[i + 1][2 * r], x[2] = acc.o[i][2 * r + 1], x[3] = acc.o[i + 1][2 * r + 1];
+                else x[0] = acc.o[i][2 * r], x[1] = acc.o[i][2 * r + 1], x[2] = x[3] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : x[e] * inv;
+                const int d0 = F8 ? 8 * i + 4 * j : 8 * i + 2 * j;
+                if (whole && F8) *reinterpret_cast<uint2*>(a.out + to * D + d0) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+                else if (whole) *reinterpret_cast<uint32_t*>(a.out + to * D + d0) = pack_bf16(x[0], x[1]);
+                else if (F8) *reinterpret_cast<float4*>(part + lr * D + d0) = make_float4(x[0], x[1], x[2], x[3]);
+                else *reinterpret_cast<float2*>(part + lr * D + d0) = make_float2(x[0], x[1]);
             }
         }
-        if (!whole && tile0 == 0)                                // the last CTA with units of this (sequence, head, group)
-            meta = make_int4((int)(((u + units) * ctas - 1) / total), seq, head, group);
-        __syncthreads();                                         // (the ring is free again)
-        u += count;
-        off += count;
-        if (off == units * per_tile) ++seq, off = 0;
     }
     if (tid == 0) a.meta[blockIdx.x] = meta;
+}
+
+// The cache's keys or values as a map of (dim, token, head, page), boxes of `box` bytes of 16 or 32 tokens.
+bool kv_map(CUtensorMap* map, const KvView& c, const uint8_t* base, bool f8, int box) {
+    const MapFns& fn = map_fns();
+    if (!fn.encode) return false;
+    const cuuint64_t size[4] = {(cuuint64_t)c.d, (cuuint64_t)c.page, (cuuint64_t)c.heads, (cuuint64_t)c.n_pages};
+    const cuuint64_t stride[3] = {(cuuint64_t)c.stride_token, (cuuint64_t)c.stride_head, (cuuint64_t)c.stride_page};
+    const cuuint32_t boxes[4] = {(cuuint32_t)(f8 ? box : box / 2), (cuuint32_t)(c.page % 32 ? 16 : 32), 1, 1}, step[4] = {1, 1, 1, 1};
+    return fn.encode(map, f8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<uint8_t*>(base), size, stride, boxes, step,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, box == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : box == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D, bool F8, int WR>
 cudaError_t attend_go(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
     using C = AttCfg<D, F8, WR>;
-    static int per_sm[64] = {0};                                 // by device
+    static bool ready[64] = {false};                             // by device
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     auto* kernel = k_kv_attend<D, F8, WR>;
-    if (!per_sm[dev]) {
-        int n = 0;
+    if (!ready[dev]) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kAttThreads, C::kSmem);
         if (e != cudaSuccess) return e;
-        per_sm[dev] = n > 0 ? n : 1;
+        ready[dev] = true;
+    }
+    // Encoding a map takes the host 2.5 us; a thread keeps the last cache's shape encoded and puts the addresses in
+    struct Kept {
+        KvView c;
+        bool set;
+        CUtensorMap map;
+    };
+    static thread_local Kept kept = {};
+    CUtensorMap k_map{}, v_map{};
+    if (a.c.page % 16 == 0) {                                    // (else no copy goes through a map)
+        const bool same = kept.set && kept.c.page == a.c.page && kept.c.heads == a.c.heads && kept.c.n_pages == a.c.n_pages &&
+                          kept.c.stride_token == a.c.stride_token && kept.c.stride_head == a.c.stride_head && kept.c.stride_page == a.c.stride_page;
+        if (!same) {
+            if (!kv_map(&kept.map, a.c, a.c.k, F8, C::kBox)) return cudaErrorInvalidValue;
+            kept.c = a.c, kept.set = true;
+        }
+        k_map = v_map = kept.map;
+        if (map_fns().replace(&k_map, a.c.k) != CUDA_SUCCESS || map_fns().replace(&v_map, a.c.v) != CUDA_SUCCESS) return cudaErrorInvalidValue;
     }
     const int64_t rows = (int64_t)a.Q * a.group, groups = (rows + 16 * WR - 1) / (16 * WR);
-    const int64_t most = (int64_t)a.c.S * a.c.heads * groups * ((kv_capacity(a.c) + C::kTile - 1) / C::kTile + 1);
-    int64_t grid = (most + C::kTeams - 1) / C::kTeams;
-    if (grid > (int64_t)num_sms() * per_sm[dev]) grid = (int64_t)num_sms() * per_sm[dev];
+    int64_t grid = (int64_t)a.c.S * a.c.heads * groups * ((kv_capacity(a.c) + kAttUnit - 1) / kAttUnit + kAttTreeUnits);
+    if (grid > num_sms()) grid = num_sms();
     if (grid > kKvMaxCtas) grid = kKvMaxCtas;
     ctas = (int)grid;
-    return launch_dependent(kernel, (unsigned)grid, kAttThreads, C::kSmem, s, a);
+    return launch_dependent(kernel, (unsigned)grid, kAttThreads, C::kSmem, s, a, k_map, v_map);
 }
 
 template <int D, bool F8>
 cudaError_t attend_rows(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
-    const int wr = kv_attend_warp_rows(a.Q * a.group);
-    return wr == 1 ? attend_go<D, F8, 1>(a, ctas, s) : wr == 2 ? attend_go<D, F8, 2>(a, ctas, s) : attend_go<D, F8, 4>(a, ctas, s);
+    const int wr = kv_attend_warp_rows(a.Q * a.group, D);
+    if constexpr (D <= 128) {
+        if (wr == 1) return attend_go<D, F8, 1>(a, ctas, s);
+        if (wr == 4) return attend_go<D, F8, 4>(a, ctas, s);
+    }
+    return attend_go<D, F8, 2>(a, ctas, s);
 }
 
 template <bool F8>

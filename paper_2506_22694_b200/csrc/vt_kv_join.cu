@@ -1,12 +1,15 @@
 // Joins the partial results of the paged attention: a (sequence, key head, group of rows) whose tokens lay in several CTAs has one partial
-// result from each, and one CTA here adds them up in the order of the tokens (so that the result does not depend on timing).
+// result from each, which are added up in the order of the tokens (so that the result does not depend on timing).
+//
+// Latency-bound: a result of 37 parts is 20 KB a row, but a chain of loads for one thread.  The rows of all joined results are dealt out as
+// tasks to a fixed grid (each CTA finds them in the list that the attention kernel left, one load and one scan), and a CTA's threads
+// share a task's parts.
 #include "vt_kv.cuh"
 
 namespace vt {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRowsPerCta = 16;
 
 __device__ __forceinline__ float exp2_of(float x) {
     float y;
@@ -21,108 +24,125 @@ __device__ __forceinline__ float4 ld_cg_f4(const float* p) {
 // weight of a part with maximum x under the common maximum m; a part of no token (maximum -inf) has l = 0 and o = 0
 __device__ __forceinline__ float weight(float x, float m) { return x == -INFINITY ? 1.0f : exp2_of(x - m); }
 
-// CTA (c, y): the result whose first part is CTA c's last, rows 16 y and on.  A thread has four dims of a row and every `gpr`-th part.
+// A thread has four dims of a row and every `share`-th part.
 __global__ void __launch_bounds__(kThreads)
-k_kv_join(const __grid_constant__ KvAttendArgs a, int warp_rows) {
-    __shared__ float s_top[kRowsPerCta];
+k_kv_join(const __grid_constant__ KvAttendArgs a, int warp_rows, int ctas) {
+    __shared__ int s_first[kKvMaxCtas];                          // CTA with the first part of each joined result, in order
+    __shared__ int s_count[kThreads / 32];
     __shared__ float4 s_o[kThreads];
-    __shared__ float s_l[kThreads];
+    __shared__ float s_l[kThreads + 64];                         // (the last seat may be a part of one)
     griddep_launch_dependents();
     griddep_wait();
-    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
-    const int last = ld_cg_s32(&a.meta[c].x);
-    if (last <= c) return;
-    const int seq = ld_cg_s32(&a.meta[c].y), head = ld_cg_s32(&a.meta[c].z), group = ld_cg_s32(&a.meta[c].w);
-    const int rows = a.Q * a.group, row0 = group * 16 * warp_rows;
-    const int lr0 = blockIdx.y * kRowsPerCta, n = min(min(rows - row0, 16 * warp_rows) - lr0, kRowsPerCta), parts = last - c + 1;
-    if (n <= 0) return;
-    const int d = a.c.d, vecs = d / 4;
-    const int64_t size = (int64_t)a.part_rows * (d + 2);
-    // part i: the second partial result of CTA c, then the first of those behind it
-    auto part = [&](int i) { return a.part + (2 * (int64_t)(c + i) + (i == 0)) * size; };
-    for (int r = tid >> 5; r < n; r += kThreads / 32) {
-        float top = -INFINITY;
-        for (int i = lane; i < parts; i += 32) top = fmaxf(top, ld_cg_f32(part(i) + (int64_t)a.part_rows * d + lr0 + r));
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int kEach = (kKvMaxCtas + kThreads - 1) / kThreads;
+    int mine = 0;
+    bool joins[kEach];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (lane == 0) s_top[r] = top;
+    for (int i = 0; i < kEach; ++i) {                            // thread t: CTAs kEach * t and on
+        const int c = kEach * tid + i;
+        joins[i] = c < ctas && ld_cg_s32(&a.meta[c].x) > c;
+        mine += joins[i];
     }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_count[warp] = incl;
     __syncthreads();
-    const int seats = kThreads / vecs;                           // rows times shares of the parts at once
-    const int gpr = n < seats ? seats / n : 1, at_once = gpr > 1 ? n : seats;
-    const int seat = tid / vecs, col = tid - seat * vecs;
-    for (int rb = 0; rb < n; rb += at_once) {
-        const int r = rb + seat / gpr, g = seat % gpr;
-        const bool live = seat < at_once * gpr && r < n;
+    int results = 0, at = incl - mine;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) at += s_count[w];
+        results += s_count[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (joins[i]) s_first[at++] = kEach * tid + i;
+    __syncthreads();
+    const int group_rows = min(a.Q * a.group, 16 * warp_rows), d = a.c.d, vecs = d / 4, seats = kThreads / vecs;
+    const int tasks = results * group_rows, each = (tasks + (int)gridDim.x - 1) / (int)gridDim.x;
+    const int at_once = min(each, seats), share = at_once ? seats / at_once : 1;
+    const int64_t size = (int64_t)a.part_rows * (d + 2);
+    const int seat = tid / vecs, col = tid - seat * vecs, which = seat / share, turn = seat - which * share;
+    for (int t0 = blockIdx.x * each; t0 < min(tasks, ((int)blockIdx.x + 1) * each); t0 += at_once) {
+        const int t = t0 + which, c = t < tasks ? s_first[t / group_rows] : 0, lr = t % group_rows;
+        const int last = ld_cg_s32(&a.meta[c].x), seq = ld_cg_s32(&a.meta[c].y), head = ld_cg_s32(&a.meta[c].z), group = ld_cg_s32(&a.meta[c].w);
+        const int row = group * 16 * warp_rows + lr, parts = last - c + 1;
+        const bool live = which < at_once && t < min(tasks, ((int)blockIdx.x + 1) * each) && row < a.Q * a.group;
+        // part i: the second partial result of CTA c, then the first of those behind it
+        auto part = [&](int i) { return a.part + (2 * (int64_t)(c + i) + (i == 0)) * size; };
         float4 o = make_float4(0, 0, 0, 0);
-        float l = 0.0f;
+        float l = 0.0f, top = -INFINITY;
         if (live) {
-            const float top = s_top[r];
-#pragma unroll 4
-            for (int i = g; i < parts; i += gpr) {
+            const float* m = a.part + (int64_t)a.part_rows * d + lr;
+            for (int i = col; i < parts; i += vecs) top = fmaxf(top, ld_cg_f32(m + (2 * (int64_t)(c + i) + (i == 0)) * size));
+        }
+        s_l[tid] = top;                                          // (the row's maximum: its seats' threads have looked at all parts)
+        __syncthreads();
+        for (int i = 0; i < vecs; ++i) top = fmaxf(top, s_l[seat * vecs + i]);
+        if (live) {
+#pragma unroll 8
+            for (int i = turn; i < parts; i += share) {
                 const float* p = part(i);
-                const float w = weight(ld_cg_f32(p + (int64_t)a.part_rows * d + lr0 + r), top);
-                const float4 x = ld_cg_f4(p + (int64_t)(lr0 + r) * d + 4 * col);
-                l += w * ld_cg_f32(p + (int64_t)a.part_rows * (d + 1) + lr0 + r);
+                const float w = weight(ld_cg_f32(p + (int64_t)a.part_rows * d + lr), top);
+                const float4 x = ld_cg_f4(p + (int64_t)lr * d + 4 * col);
+                l += w * ld_cg_f32(p + (int64_t)a.part_rows * (d + 1) + lr);
                 o.x += w * x.x, o.y += w * x.y, o.z += w * x.z, o.w += w * x.w;
             }
         }
-        if (gpr > 1) {
-            s_o[tid] = o, s_l[tid] = l;
-            __syncthreads();
-            if (live && g == 0)
-                for (int i = 1; i < gpr; ++i) {
-                    const float4 x = s_o[tid + i * vecs];
-                    o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
-                    l += s_l[tid + i * vecs];
-                }
-        }
-        if (live && g == 0) {
-            const int row = row0 + lr0 + r, qi = row / a.group;
-            const int64_t at = ((int64_t)seq * a.Q + qi) * a.Hq + head * a.group + (row - qi * a.group);
+        __syncthreads();
+        s_o[tid] = o, s_l[tid] = l;
+        __syncthreads();
+        if (live && turn == 0) {
+            for (int i = 1; i < share; ++i) {
+                const float4 x = s_o[tid + i * vecs];
+                o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+                l += s_l[tid + i * vecs];
+            }
+            const int qi = row / a.group;
+            const int64_t to = ((int64_t)seq * a.Q + qi) * a.Hq + head * a.group + (row - qi * a.group);
             const bool none = l == 0.0f;
             const float inv = none ? 0.0f : 1.0f / l;
             const __nv_bfloat162 x = none ? __floats2bfloat162_rn(0, 0) : __floats2bfloat162_rn(o.x * inv, o.y * inv);
             const __nv_bfloat162 y = none ? __floats2bfloat162_rn(0, 0) : __floats2bfloat162_rn(o.z * inv, o.w * inv);
-            *reinterpret_cast<uint2*>(a.out + at * d + 4 * col) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-            if (col == 0 && a.lse) a.lse[at] = none ? -INFINITY : (s_top[r] + log2f(l)) * 0.6931471805599453f;
+            *reinterpret_cast<uint2*>(a.out + to * d + 4 * col) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+            if (col == 0 && a.lse) a.lse[to] = none ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
         }
+        __syncthreads();                                         // (the sums have been read)
     }
 }
 
 }  // namespace
 
-int kv_attend_warp_rows(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+// (heads over 128: two always, eight teams would leave no room for a tile each)
+int kv_attend_warp_rows(int rows, int d) { return d > 128 ? 2 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
-static int part_rows(int rows) { return rows < 16 * kv_attend_warp_rows(rows) ? rows : 16 * kv_attend_warp_rows(rows); }
+static int part_rows(int rows, int d) { return rows < 16 * kv_attend_warp_rows(rows, d) ? rows : 16 * kv_attend_warp_rows(rows, d); }
 
 size_t kv_attend_scratch_bytes(int rows, int d) {
-    const size_t parts = (size_t)kKvMaxCtas * 2 * ((part_rows(rows) + 3) & ~3) * (d + 2) * sizeof(float);
+    const size_t parts = (size_t)kKvMaxCtas * 2 * ((part_rows(rows, d) + 3) & ~3) * (d + 2) * sizeof(float);
     return align_up(kKvMaxCtas * sizeof(int4), 256) + parts;
 }
 
 void kv_attend_carve(KvAttendArgs& a, uint8_t* scratch) {
     a.meta = reinterpret_cast<int4*>(scratch);
     a.part = reinterpret_cast<float*>(scratch + align_up(kKvMaxCtas * sizeof(int4), 256));
-    a.part_rows = (part_rows(a.Q * a.group) + 3) & ~3;           // (a part is a whole number of 16-byte vectors)
+    a.page_shift = -1;
+    for (int i = 0; i < 31; ++i)
+        if (a.c.page == 1 << i) a.page_shift = i;
+    a.box = a.c.page % 32 == 0 ? 32 : a.c.page % 16 == 0 ? 16 : 0;
+    a.part_rows = (part_rows(a.Q * a.group, a.c.d) + 3) & ~3;           // (a part is a whole number of 16-byte vectors)
 }
 
 cudaError_t launch_kv_attend(const KvAttendArgs& a, cudaStream_t s) {
     int ctas = 0;
     const cudaError_t e = a.c.k_exp ? launch_kv_attend_e4m3(a, ctas, s) : launch_kv_attend_bf16(a, ctas, s);
     if (e != cudaSuccess) return e;
-    const int wr = kv_attend_warp_rows(a.Q * a.group);
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)ctas, (unsigned)((a.part_rows + kRowsPerCta - 1) / kRowsPerCta));
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    count_launch();
-    return cudaLaunchKernelEx(&cfg, k_kv_join, a, wr);
+    const int wr = kv_attend_warp_rows(a.Q * a.group, a.c.d);
+    const unsigned grid = (unsigned)(2 * num_sms());
+    return launch_dependent(k_kv_join, grid, kThreads, 0, s, a, wr, ctas);
 }
 
 }  // namespace vt

@@ -1,39 +1,14 @@
 // Tensor-core plumbing shared by the two head kernels: mbarrier and TMA wrappers, tcgen05 operand and
 // instruction descriptors, and the host-side encoding of the tensor maps.
 #pragma once
-#include <cuda.h>
-
-#include <mutex>
-
-#include "vt_common.cuh"
+#include "vt_maps.cuh"
+#include "vt_mbar.cuh"
 
 namespace vt {
 namespace {
 
 constexpr int kBK = 64;                   // columns of d per tensor copy: 128 bytes, one swizzle row
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint64_t* b, int count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint64_t* b, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint64_t* b, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-        : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long global_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
 // One lane of a converged warp.  The single-thread roles (copy producer, MMA issuer) are entered through this and
 // not through `lane == 0`: behind elect.sync the compiler knows that one thread is active and hands tcgen05 and
 // copy instructions their operands in uniform registers; behind a comparison it guards every one of them against
@@ -89,34 +64,6 @@ __host__ __device__ constexpr uint32_t make_idesc(int M, int N) {
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-typedef CUresult (*ReplaceAddressFn)(CUtensorMap*, void*);
-
-struct MapFns {
-    EncodeTiledFn encode;
-    ReplaceAddressFn replace;
-};
-
-const MapFns& map_fns() {
-    static std::mutex mu;
-    static MapFns fns{nullptr, nullptr};
-    std::lock_guard<std::mutex> lock(mu);
-    if (!fns.encode) {
-        void *e = nullptr, *r = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapReplaceAddress", &r, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fns.replace = reinterpret_cast<ReplaceAddressFn>(r);
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &e, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess && fns.replace)
-            fns.encode = reinterpret_cast<EncodeTiledFn>(e);
-    }
-    return fns;
-}
-
 // bf16 matrix [rows, cols] row-major -> boxes of kBK columns x box_rows rows, 128-byte swizzle; with steps > 0 boxes of
 // `steps` of those behind one another, as a third dimension (cols a multiple of kBK).  Encoding a map
 // takes the host about 2.5 us, two of them 5 of a call's 12; the last few shapes of a thread are kept encoded (a

@@ -109,6 +109,11 @@ class Host:
                 out.append(decode(rows, ex))
         return out
 
+    def powers(self, s, index):
+        """The values' powers of two [n, heads] (e4m3)."""
+        e = torch.stack([self.ve[p, :, j] for p, j in (self.place(s, i) for i in index)])
+        return torch.pow(torch.tensor(2.0, dtype=torch.float64), (e.long() - 127).double())
+
     def same(self, dev=None):
         """Whether the device's cache holds the host's bytes."""
         for a, b in zip((self.k, self.v, self.ke, self.ve), dev or self.dev):
@@ -125,8 +130,9 @@ def attend(host, q, lens, Q, node=None, parent=None, scale=None):
     """(out, lse, bound of |out's error|, bound of |lse's error|), in 64 bits.
 
     The bounds: a score is a sum of d products in fp32 (each addition off by at most a step, 2^-23 of the sum of magnitudes so far), an
-    exponential by 2^-21, a weight as two bf16 pieces by 2^-17; a relative error of the weights moves their mean by at most twice that of the
-    mean magnitude; sums over n tokens add n steps of 2^-23; the result is rounded to bf16 (2^-8) and parts are joined with a few more
+    exponential by 2^-21, a weight as two bf16 pieces by 2^-17 or (e4m3) as one of f16 by 2^-11, and there, where it is under 2^-14 of the
+    largest weight times power, by 2^-25 of that, times a value of 448 at the most; a relative error of the weights moves their mean by at
+    most twice that of the mean magnitude; sums over n tokens add n steps of 2^-23; the result is rounded to bf16 (2^-8) and parts are joined with a few more
     exponentials (2^-20 in all)."""
     T, Hq, d = q.shape
     S, g = host.S, Hq // host.heads
@@ -159,8 +165,9 @@ def attend(host, q, lens, Q, node=None, parent=None, scale=None):
                 out[t, h] = (p[:, None] * v[:, h // g]).sum(0) / p.sum()
                 lse[t, h] = m + torch.log(p.sum())
                 mean = (p[:, None] * v[:, h // g].abs()).sum(0) / p.sum()
-                delta = 2.0 ** -17 + 2.0 ** -20 + worst
-                tol[t, h] = 2.0 ** -8 * out[t, h].abs() + (2 * delta + len(seen) * 2.0 ** -23) * mean * (1 + 2.0 ** -7) + 1e-37
+                delta = (2.0 ** -11 if host.e4m3 else 2.0 ** -17) + 2.0 ** -20 + worst
+                small = 2.0 ** -25 * 448 * len(seen) * float((p * host.powers(s, seen)[:, h // g]).max() / p.sum()) if host.e4m3 else 0.0
+                tol[t, h] = 2.0 ** -8 * out[t, h].abs() + (2 * delta + len(seen) * 2.0 ** -23) * mean * (1 + 2.0 ** -7) + small + 1e-37
                 tol_l[t, h] = worst + 2.0 ** -20 + len(seen) * 2.0 ** -23 + 2.0 ** -22 * abs(float(lse[t, h]))
     return out, lse, tol, tol_l
 
