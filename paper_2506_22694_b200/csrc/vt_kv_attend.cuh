@@ -37,7 +37,10 @@ constexpr int kAttThreads = 32 * (kAttWarps + kAttFeeds);
 constexpr int kAttConsumerRegs = 200, kAttProducerRegs = 104;
 static_assert(kAttWarps * kAttConsumerRegs + kAttFeeds * kAttProducerRegs <= (kAttWarps + kAttFeeds) * 168, "what the block was launched with");
 constexpr int kAttUnit = 64;                                     // tokens
-constexpr int kAttTreeUnits = 2;                                 // what a tree's tokens count for when the work is dealt out
+// What a result counts for besides its tokens when the work is dealt out (the walk to it, its queries, the meeting), and a tree's tokens.
+constexpr int kAttPairUnits = 2, kAttTreeUnits = 2;
+constexpr int kAttSnap = 2;                                      // no result is split so near to its ends
+constexpr int kAttLens = 1024;                                   // sequences whose lengths are kept in shared memory
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
 constexpr int kAttRound = kAttTile * kAttFeeds;                  // tokens that the producers look up at a time
 constexpr unsigned long long kAttWaitNs = 2000000000ull;         // bound of a wait on a tile or a place in the ring
@@ -60,7 +63,7 @@ struct AttCfg {
     static constexpr int kQPitch = 2 * D + 16;
     static constexpr int kQBytes = kQRegs ? 0 : WR * 16 * kQPitch;
     static constexpr int kMeet = kAttWarps / 2 * (D / 8 + 1) * 512;   // where the teams' results meet: D / 8 + 1 vectors of each lane of half of them
-    static constexpr int kParents = 2 * kKvMaxNodes;
+    static constexpr int kParents = 2 * kKvMaxNodes + 4 * kAttLens;                        // ... and the lengths
     static constexpr int kFree = 226 * 1024 - 2048 - kQBytes - kMeet - kParents;
     // A ring of kPer places for each producer.  Its tiles go to the teams in turn, and a place is always of the same team: who waits for a turn
     // of a place has waited for every turn before, and cannot take the next but one, of the same parity, for its own.
@@ -397,19 +400,19 @@ __device__ __forceinline__ int att_len(const KvAttendArgs& a, int s) {
     return (int)min((int64_t)max(ld_cg_s32(a.lens + s), 0), (int64_t)a.c.max_pages * a.c.page);
 }
 __device__ __forceinline__ int att_units(const KvAttendArgs& a, int len) {
-    return max((len + kAttUnit - 1) / kAttUnit + (a.node ? kAttTreeUnits : 0), 1);
+    return (len + kAttUnit - 1) / kAttUnit + kAttPairUnits + (a.node ? kAttTreeUnits : 0);
 }
-__device__ __forceinline__ bool att_next(const KvAttendArgs& a, int groups, AttWalk& w, AttSegment& g) {
+__device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens, int groups, AttWalk& w, AttSegment& g) {
     if (w.u >= w.u1) return false;
     g.seq = w.seq;
-    g.len = att_len(a, g.seq);
+    g.len = g.seq < kAttLens ? lens[g.seq] : att_len(a, g.seq);
     g.units = att_units(a, g.len);
     const int pair = (int)(w.off / g.units);
     g.tile0 = (int)(w.off - (long long)pair * g.units);
     g.count = (int)min((long long)(g.units - g.tile0), w.u1 - w.u);
     g.head = pair / groups, g.group = pair - g.head * groups;
-    g.token = (int)min((long long)g.tile0 * kAttUnit, (long long)g.len);
-    g.token_end = (int)min((long long)(g.tile0 + g.count) * kAttUnit, (long long)g.len);
+    g.token = (int)min((long long)max(g.tile0 - kAttPairUnits, 0) * kAttUnit, (long long)g.len);
+    g.token_end = (int)min((long long)max(g.tile0 + g.count - kAttPairUnits, 0) * kAttUnit, (long long)g.len);
     g.tree = a.node && g.tile0 + g.count == g.units;
     w.u += g.count, w.off += g.count;
     if (w.off == (long long)g.units * a.c.heads * groups) ++w.seq, w.off = 0;
@@ -435,6 +438,7 @@ struct AttProducer {
     uint64_t *full, *empty;
     int16_t* parents;
     volatile int* dead;
+    const int* lens;
     AttWalk walk;
     AttSegment g;
     int groups, lane, feed;
@@ -448,7 +452,7 @@ struct AttProducer {
     // last; with more teams than producers the last two rounds are, if need be one of no tokens.
     __device__ bool token(int32_t& index, AttToken& r, int& seq) {
         if (mode == 0) {
-            if (!att_next(a, groups, walk, g)) return false;
+            if (!att_next(a, lens, groups, walk, g)) return false;
             mode = g.token >= g.token_end && g.tree ? 2 : 1;
             told = false;
             if (g.tree) load_tree();
@@ -735,12 +739,13 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     __shared__ uint64_t s_full[C::kSlots], s_empty[C::kSlots];
     __shared__ float s_qscale[C::kQRegs ? 1 : 16 * WR];          // powers that the queries' rows were scaled by, undone in the scores
     __shared__ long long s_sum[kAttWarps + kAttFeeds];
-    __shared__ long long s_at;
-    __shared__ int s_seq, s_dead;
+    __shared__ long long s_at[2], s_u[2];
+    __shared__ int s_seq[2], s_dead;
     uint8_t* notes = ring + C::kSlots * C::kSlot;
     uint8_t* qs = notes + C::kSlots * C::kNote;
     float4* meet = reinterpret_cast<float4*>(qs + C::kQBytes);
     int16_t* parents = reinterpret_cast<int16_t*>(qs + C::kQBytes + C::kMeet);
+    int* lens = reinterpret_cast<int*>(parents + kKvMaxNodes);   // of the first kAttLens sequences
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid < C::kSlots) {
         mbar_init(s_full + tid, 1);                              // the producer's word that all but its copies is there
@@ -756,7 +761,11 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     // this CTA's run of units: [u0, u1) of all sequences' units laid end to end
     const int chunk = (a.c.S + kAttThreads - 1) / kAttThreads, sa = min(tid * chunk, a.c.S), sb = min(sa + chunk, a.c.S);
     long long mine = 0;
-    for (int s = sa; s < sb; ++s) mine += att_units(a, att_len(a, s));
+    for (int s = sa; s < sb; ++s) {
+        const int n = att_len(a, s);
+        if (s < kAttLens) lens[s] = n;
+        mine += att_units(a, n);
+    }
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -774,35 +783,44 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     before *= per_unit;
     mine *= per_unit;
     const long long ctas = min((long long)gridDim.x, total);
-    const bool idle = blockIdx.x >= ctas;
-    if (idle) {
+    // The run begins and ends where equal shares do, but not within a result's first or last units: a piece that small would cost more than its
+    // tokens.  One thread's sequences hold either border.
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const long long border = blockIdx.x < ctas ? total * (blockIdx.x + i) / ctas : total;
+        if (border == total) {
+            if (tid == 0) s_seq[i] = a.c.S, s_at[i] = 0, s_u[i] = total;
+        } else if (border >= before && border < before + mine) {
+            long long at = before, n = 0;
+            int s = sa, units = 0;
+            for (;; ++s) {
+                units = att_units(a, s < kAttLens ? lens[s] : att_len(a, s));
+                n = units * per_unit;
+                if (s == sb - 1 || at + n > border) break;
+                at += n;
+            }
+            long long off = border - at;
+            const int in = (int)(off % units);
+            if (in <= kAttPairUnits + kAttSnap) off -= in;
+            else if (in >= units - kAttSnap) off += units - in;
+            s_u[i] = at + off;
+            if (off == n) ++s, off = 0;
+            s_seq[i] = s, s_at[i] = off;
+        }
+    }
+    __syncthreads();
+    AttWalk walk;
+    walk.u = s_u[0], walk.u1 = s_u[1], walk.seq = s_seq[0], walk.off = s_at[0];
+    if (walk.u >= walk.u1) {
         if (tid == 0) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
         return;
     }
-    AttWalk walk;
-    walk.u = total * blockIdx.x / ctas;
-    walk.u1 = total * (blockIdx.x + 1) / ctas;
-    if (walk.u >= before && walk.u < before + mine) {            // one thread's sequences hold the first unit
-        long long at = before;
-        int s = sa;
-        while (s < sb - 1) {
-            const long long n = att_units(a, att_len(a, s)) * per_unit;
-            if (at + n > walk.u) break;
-            at += n;
-            ++s;
-        }
-        s_seq = s;
-        s_at = walk.u - at;
-    }
-    __syncthreads();
-    walk.seq = s_seq;
-    walk.off = s_at;
 
     if (warp >= kAttWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAttProducerRegs));
         const int feed = warp - kAttWarps;
         AttProducer<D, F8, WR> p{a, &k_map, &v_map, ring + feed * C::kPer * C::kSlot, notes + feed * C::kPer * C::kNote, s_full + feed * C::kPer,
-                                 s_empty + feed * C::kPer, parents, &s_dead, walk, {}, groups, lane, feed, 0, false, -1, -1, -1, -1, -1};
+                                 s_empty + feed * C::kPer, parents, &s_dead, lens, walk, {}, groups, lane, feed, 0, false, -1, -1, -1, -1, -1};
         p.run();
         return;
     }
@@ -816,7 +834,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     AttSegment g, after;
     AttQueries<D, F8, WR> q;
     long long at = walk.u;
-    att_next(a, groups, walk, g);
+    att_next(a, lens, groups, walk, g);
     q.fetch(a, g, warp, lane);
     for (bool go_on = true; go_on; g = after) {
         const int row0 = g.group * 16 * WR;
@@ -849,7 +867,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         }
 
         const long long at_next = walk.u;
-        go_on = att_next(a, groups, walk, after);
+        go_on = att_next(a, lens, groups, walk, after);
         if (go_on) q.fetch(a, after, warp, lane);                // (on their way while the results meet)
         if (WR == 4) feed = team;
 
@@ -888,8 +906,8 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             }
         }
         const bool whole = g.count == g.units;
-        if (!whole && g.tile0 == 0)                              // the last CTA with units of this (sequence, head, group)
-            meta = make_int4((int)(((at + g.units) * ctas - 1) / total), g.seq, g.head, g.group);
+        if (!whole && g.tile0 == 0)                              // the last CTA whose run begins within this result
+            meta = make_int4((int)(((at + g.units - kAttSnap) * ctas - 1) / total), g.seq, g.head, g.group);
         at = at_next;
         if (team != 0) continue;
         const bool broken = *const_cast<volatile int*>(&s_dead) != 0;
@@ -977,7 +995,7 @@ cudaError_t attend_go(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
         if (map_fns().replace(&k_map, a.c.k) != CUDA_SUCCESS || map_fns().replace(&v_map, a.c.v) != CUDA_SUCCESS) return cudaErrorInvalidValue;
     }
     const int64_t rows = (int64_t)a.Q * a.group, groups = (rows + 16 * WR - 1) / (16 * WR);
-    int64_t grid = (int64_t)a.c.S * a.c.heads * groups * ((kv_capacity(a.c) + kAttUnit - 1) / kAttUnit + kAttTreeUnits);
+    int64_t grid = (int64_t)a.c.S * a.c.heads * groups * ((kv_capacity(a.c) + kAttUnit - 1) / kAttUnit);
     if (grid > num_sms()) grid = num_sms();
     if (grid > kKvMaxCtas) grid = kKvMaxCtas;
     ctas = (int)grid;
