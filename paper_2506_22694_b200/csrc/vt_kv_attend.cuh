@@ -42,7 +42,8 @@ constexpr int kAttPairUnits = 2, kAttTreeUnits = 2;
 constexpr int kAttSnap = 2;                                      // no result is split so near to its ends
 constexpr int kAttLens = 1024;                                   // sequences whose lengths are kept in shared memory
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
-constexpr int kAttRound = kAttTile * kAttFeeds;                  // tokens that the producers look up at a time
+constexpr int kAttTurns = 2;                                     // tiles of a producer in a round
+constexpr int kAttRound = kAttTile * kAttFeeds * kAttTurns;      // tokens that the producers look up at a time
 constexpr unsigned long long kAttWaitNs = 2000000000ull;         // bound of a wait on a tile or a place in the ring
 
 template <int D, bool F8, int WR>
@@ -65,8 +66,9 @@ struct AttCfg {
     static constexpr int kMeet = kAttWarps / 2 * (D / 8 + 1) * 512;   // where the teams' results meet: D / 8 + 1 vectors of each lane of half of them
     static constexpr int kParents = 2 * kKvMaxNodes + 4 * kAttLens;                        // ... and the lengths
     static constexpr int kFree = 226 * 1024 - 2048 - kQBytes - kMeet - kParents;
-    // A ring of kPer places for each producer.  Its tiles go to the teams in turn, and a place is always of the same team: who waits for a turn
-    // of a place has waited for every turn before, and cannot take the next but one, of the same parity, for its own.
+    // A ring of kPer places for each producer.  Tile 4 t + p of a round is producer p's in turn t, and goes to team (4 t + p) mod teams; a place is
+    // always of the same team: who waits for a turn of a place has waited for every turn before, and cannot take the next but one, of the same
+    // parity, for its own.
     static constexpr int kShare = kTeams > kAttFeeds ? kTeams / kAttFeeds : 1;             // teams of a ring
     static constexpr int kPer = (kFree / (kSlot + kNote) < 40 ? kFree / (kSlot + kNote) : 40) / kAttFeeds / kShare * kShare;
     static constexpr int kSlots = kAttFeeds * kPer;
@@ -90,11 +92,15 @@ __device__ __forceinline__ bool elect_lane() {
     asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
     return r != 0;
 }
+// 16 bytes, or zeros where `have` is false (then the source is not read)
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool have) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
+}
 // a box of the cache's map: dim x, token, head, page
-__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap* map, int x, int token, int head, int page, uint64_t* bar) {
+__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap* map, int x, int token, int head, int page, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-        ::"r"(dst), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(smem_u32(bar)) : "memory");
+        ::"r"(dst), "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(bar) : "memory");
 }
 // orders this thread's stores to shared memory in front of later bulk copies into the same place
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -163,15 +169,35 @@ __device__ __forceinline__ void consumers_barrier() { asm volatile("bar.sync 15,
 
 __device__ __forceinline__ void feeds_barrier() { asm volatile("bar.sync 14, %0;" ::"n"(32 * kAttFeeds) : "memory"); }
 
+// The mbarriers by their addresses in shared memory: 32 bits, of which the warps here keep many.
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {       // without arriving
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void st_shared(uint32_t at, const uint4& x) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+__device__ __forceinline__ void st_shared(uint32_t at, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory"); }
+__device__ __forceinline__ uint32_t ld_shared(uint32_t at) {
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    return x;
+}
+
 // A wait within the CTA (nothing here waits for another).  Where it runs out, the flag makes all later waits return at once, every loop still
 // ends, and the results are no numbers.
-__device__ __forceinline__ void att_wait(uint64_t* bar, uint32_t parity, volatile int* dead, Ctrl* ctrl) {
-    if (mbar_try(bar, parity)) return;
+__device__ __forceinline__ void att_wait(uint32_t bar, uint32_t parity, uint32_t dead, Ctrl* ctrl) {
+    if (bar_try(bar, parity)) return;
     const unsigned long long t0 = global_ns();
-    while (!mbar_try(bar, parity)) {
-        if (*dead) return;
+    while (!bar_try(bar, parity)) {
+        if (ld_shared(dead)) return;
         if (global_ns() - t0 > kAttWaitNs) {
-            *dead = 1;
+            st_shared(dead, 1u);
             atomicOr(&ctrl->flags, (uint32_t)VT_FLAG_TIMEOUT);
             return;
         }
@@ -419,14 +445,13 @@ __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens,
     return true;
 }
 
-// A producer's lane: a token of its tile.
-struct AttToken {
-    int32_t id, in;               // page (-1: out of range, -2: no token) and place in it
-    int head, flags;              // header of the tile
-    bool some;                    // the tile has tokens
-    bool have;                    // the round exists
-    unsigned long long mask;      // a tree's token: the rows that see it
-    uint32_t ke, ve;              // e4m3: its exponents' bytes
+// A producer's lane: its tokens of a round, one of each tile.
+struct AttTokens {
+    int32_t id[kAttTurns], in[kAttTurns];                        // page (-1: out of range, -2: no token) and place in it
+    unsigned long long mask[kAttTurns];                          // a tree's token: the rows that see it
+    uint32_t ke[kAttTurns], ve[kAttTurns];                       // e4m3: its exponents' bytes
+    int head, n;                                                 // tokens of the round
+    bool tree, last, have;                                       // the segment ends with it; it exists
 };
 
 template <int D, bool F8, int WR>
@@ -434,60 +459,63 @@ struct AttProducer {
     using C = AttCfg<D, F8, WR>;
     const KvAttendArgs& a;
     const CUtensorMap *k_map, *v_map;
-    uint8_t *ring, *notes;        // of this producer
-    uint64_t *full, *empty;
+    uint32_t ring, notes, full, empty, dead;                     // of this producer, in shared memory
     int16_t* parents;
-    volatile int* dead;
     const int* lens;
     AttWalk walk;
     AttSegment g;
     int groups, lane, feed;
-    int mode;                     // 0: the next segment, 1: committed tokens, 2: the tree's, 3: a round of none
-    bool told;                    // the round before has told its teams that it was their last
+    int mode;                     // 0: the next segment, 1: committed tokens, 2: the tree's
     int tree_of, n0, n1, f0, f1;  // whose parents are here; nodes of rows lane and lane + 32, and where they have got to
     int place = 0, filled = 0;    // of the next tile, in the ring; tiles so far
     uint32_t parity = 1;          // (an empty ring's places count as given back)
+    unsigned long long dirty = 0; // places that hold rows which threads have stored
 
-    // This lane's token of the next round: its place in the sequence; false: no more rounds.  Every team is told which tile of a segment is its
-    // last; with more teams than producers the last two rounds are, if need be one of no tokens.
-    __device__ bool token(int32_t& index, AttToken& r, int& seq) {
+    __device__ int mine(int turn) const { return kAttTile * (kAttFeeds * turn + feed) + lane; }      // which of a round's tokens
+
+    // a lane's tokens of the next round -> their page ids (the loads are left in flight)
+    __device__ void look_up(AttTokens& r) {
         if (mode == 0) {
-            if (!att_next(a, lens, groups, walk, g)) return false;
+            r.have = att_next(a, lens, groups, walk, g);
+            if (!r.have) return;
             mode = g.token >= g.token_end && g.tree ? 2 : 1;
-            told = false;
             if (g.tree) load_tree();
         }
-        seq = g.seq, r.head = g.head;
-        r.flags = 0, r.mask = 0, index = -1;
-        bool last = mode == 3, before_last = false;
-        int n = 0;                                               // tokens of the round
+        r.have = true, r.head = g.head, r.tree = mode == 2;
+        int index[kAttTurns];
+#pragma unroll
+        for (int t = 0; t < kAttTurns; ++t) index[t] = -1, r.mask[t] = 0;
         if (mode == 1) {
-            n = min(g.token_end - g.token, kAttRound);
-            const int t = kAttTile * feed + lane;
-            if (t < n) index = g.token + t;
-            g.token += n;
-            last = g.token >= g.token_end && !g.tree;
-            before_last = g.token < g.token_end && g.token + kAttRound >= g.token_end && !g.tree;
-            if (g.token >= g.token_end && g.tree) mode = 2;
-        } else if (mode == 2) {
+            r.n = min(g.token_end - g.token, kAttRound);
+#pragma unroll
+            for (int t = 0; t < kAttTurns; ++t)
+                if (mine(t) < r.n) index[t] = g.token + mine(t);
+            g.token += r.n;
+            r.last = g.token >= g.token_end && !g.tree;
+            if (g.token >= g.token_end) mode = g.tree ? 2 : 0;
+        } else {
             // the nodes that some row sees, largest first: the rows' walks to the root are merged (by every producer, for its own tokens)
-            r.flags = kAttTree;
-            for (; n < kAttRound; ++n) {
+            for (r.n = 0; r.n < kAttRound; ++r.n) {
                 const int f = __reduce_max_sync(0xffffffffu, max(f0, f1));
                 if (f < 0) break;
                 const unsigned lo = __ballot_sync(0xffffffffu, f0 == f), hi = __ballot_sync(0xffffffffu, f1 == f);
-                if (n == kAttTile * feed + lane) index = (int32_t)min((int64_t)g.len + f, (int64_t)INT32_MAX), r.mask = ((unsigned long long)hi << 32) | lo;
+#pragma unroll
+                for (int t = 0; t < kAttTurns; ++t)
+                    if (r.n == mine(t)) index[t] = (int32_t)min((int64_t)g.len + f, (int64_t)INT32_MAX), r.mask[t] = ((unsigned long long)hi << 32) | lo;
                 const int up = a.parent ? (int)parents[f] : f - 1;
                 f0 = f0 == f ? up : f0, f1 = f1 == f ? up : f1;
             }
-            last = __reduce_max_sync(0xffffffffu, max(f0, f1)) < 0;
+            r.last = __reduce_max_sync(0xffffffffu, max(f0, f1)) < 0;
+            if (r.last) mode = 0;
         }
-        r.some = kAttTile * feed < n;
-        if (last) mode = mode == 3 || told || C::kShare == 1 ? 0 : 3;
-        told = before_last && C::kShare > 1;
-        // (of two tiles of a round the second is the team's last)
-        if ((last && (WR < 4 || feed >= 2)) || told) r.flags |= kAttEnd;
-        return true;
+#pragma unroll
+        for (int t = 0; t < kAttTurns; ++t) {
+            r.id[t] = -2, r.in[t] = 0;
+            if (index[t] < 0) continue;
+            const uint32_t page = a.page_shift >= 0 ? (uint32_t)index[t] >> a.page_shift : (uint32_t)index[t] / (uint32_t)a.c.page;
+            r.in[t] = index[t] - (int32_t)(page * (uint32_t)a.c.page);
+            r.id[t] = page < (uint32_t)a.c.max_pages ? ld_cg_s32(a.c.pages + (int64_t)g.seq * a.c.pages_ld + page) : -1;
+        }
     }
 
     __device__ void load_tree() {
@@ -512,121 +540,123 @@ struct AttProducer {
         f0 = n0, f1 = n1;
     }
 
-    // a lane's token -> its page id (the load is left in flight)
-    __device__ void look_up(AttToken& p) {
-        int32_t index;
-        int seq = 0;
-        p.have = token(index, p, seq);
-        p.id = -2, p.in = 0;
-        if (!p.have || index < 0) return;
-        const uint32_t page = a.page_shift >= 0 ? (uint32_t)index >> a.page_shift : (uint32_t)index / (uint32_t)a.c.page;
-        p.in = index - (int32_t)(page * (uint32_t)a.c.page);
-        p.id = page < (uint32_t)a.c.max_pages ? ld_cg_s32(a.c.pages + (int64_t)seq * a.c.pages_ld + page) : -1;
-    }
-    // page id -> exponents (left in flight, too)
-    __device__ void resolve(AttToken& p) {
-        if (p.id != -2 && (uint32_t)p.id >= (uint32_t)a.c.n_pages) {
-            kv_flag(a.ctrl);
-            p.id = -2;
-        }
-        p.ke = p.ve = 0;
-        if (F8 && p.id >= 0) {
-            const int64_t e = ((int64_t)p.id * a.c.heads + p.head) * a.c.page + p.in;
-            asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(p.ke) : "l"(a.c.k_exp + e) : "memory");
-            asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(p.ve) : "l"(a.c.v_exp + e) : "memory");
+    // page ids -> exponents (left in flight, too)
+    __device__ void resolve(AttTokens& r) {
+#pragma unroll
+        for (int t = 0; t < kAttTurns; ++t) {
+            if (r.id[t] != -2 && (uint32_t)r.id[t] >= (uint32_t)a.c.n_pages) {
+                kv_flag(a.ctrl);
+                r.id[t] = -2;
+            }
+            if (F8) {
+                const int64_t e = r.id[t] >= 0 ? ((int64_t)r.id[t] * a.c.heads + r.head) * a.c.page + r.in[t] : 0;
+                asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(r.ke[t]) : "l"(a.c.k_exp + e) : "memory");
+                asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(r.ve[t]) : "l"(a.c.v_exp + e) : "memory");
+            }
         }
     }
 
-    __device__ void emit(const AttToken& r) {
-        uint8_t *tile = ring + place * C::kSlot, *note = notes + place * C::kNote;
-        att_wait(empty + place, parity, dead, a.ctrl);
-        if (r.some) {
-            const bool ok = r.id >= 0;
-            const unsigned have = __ballot_sync(0xffffffffu, ok);
-            // 16 or 32 tokens of a page at a time by tensor copies, where they are all there
-            unsigned boxed = 0;                                  // tokens that come so
-            if (a.box == 32 && have == 0xffffffffu && !(r.flags & kAttTree)) boxed = have;
-            else if (a.box == 16 && !(r.flags & kAttTree)) boxed = ((have & 0xffffu) == 0xffffu ? 0xffffu : 0u) | ((have >> 16) == 0xffffu ? 0xffff0000u : 0u);
-            if (boxed) {
-                const int id0 = __shfl_sync(0xffffffffu, r.id, 0), in0 = __shfl_sync(0xffffffffu, r.in, 0);
-                const int id1 = __shfl_sync(0xffffffffu, r.id, 16), in1 = __shfl_sync(0xffffffffu, r.in, 16);
-                if (elect_lane()) {
-                    uint64_t* bar = full + place;
-                    mbar_expect(bar, __popc(boxed) * 2 * C::kRow);
-                    const uint32_t dst = smem_u32(tile);
+    // A tile's rows.  16 or 32 tokens of a page at a time come by tensor copies, where they are all there.
+    __device__ void copy(const AttTokens& r, int turn, int at) {
+        const uint32_t tile = ring + at * C::kSlot, bar = full + 8 * at;
+        const int32_t id = r.id[turn], in = r.in[turn];
+        const unsigned have = __ballot_sync(0xffffffffu, id >= 0);
+        unsigned boxed = 0;                                      // tokens that come so
+        if (!r.tree && a.box == 32) boxed = have == 0xffffffffu ? have : 0u;
+        else if (!r.tree && a.box == 16) boxed = ((have & 0xffffu) == 0xffffu ? 0xffffu : 0u) | ((have >> 16) == 0xffffu ? 0xffff0000u : 0u);
+        if (boxed) {
+            const int id0 = __shfl_sync(0xffffffffu, id, 0), in0 = __shfl_sync(0xffffffffu, in, 0);
+            const int id1 = __shfl_sync(0xffffffffu, id, 16), in1 = __shfl_sync(0xffffffffu, in, 16);
+            if (elect_lane()) {
+                if (dirty >> at & 1) fence_async();              // (what threads have stored there comes first)
+                bar_expect(bar, __popc(boxed) * 2 * C::kRow);
 #pragma unroll
-                    for (int x = 0; x < C::kRow / C::kBox; ++x) {
-                        const uint32_t to = dst + x * C::kTile * C::kBox;
-                        const int dim = x * (F8 ? C::kBox : C::kBox / 2);
-                        if (boxed & 1u) {
-                            box_copy(to, k_map, dim, in0, r.head, id0, bar);
-                            box_copy(to + C::kHalf, v_map, dim, in0, r.head, id0, bar);
-                        }
-                        if (a.box == 16 && (boxed >> 31)) {
-                            box_copy(to + 16 * C::kBox, k_map, dim, in1, r.head, id1, bar);
-                            box_copy(to + C::kHalf + 16 * C::kBox, v_map, dim, in1, r.head, id1, bar);
-                        }
+                for (int x = 0; x < C::kRow / C::kBox; ++x) {
+                    const uint32_t to = tile + x * C::kTile * C::kBox;
+                    const int dim = x * (F8 ? C::kBox : C::kBox / 2);
+                    if (boxed & 1u) {
+                        box_copy(to, k_map, dim, in0, r.head, id0, bar);
+                        box_copy(to + C::kHalf, v_map, dim, in0, r.head, id0, bar);
+                    }
+                    if (a.box == 16 && (boxed >> 31)) {
+                        box_copy(to + 16 * C::kBox, k_map, dim, in1, r.head, id1, bar);
+                        box_copy(to + C::kHalf + 16 * C::kBox, v_map, dim, in1, r.head, id1, bar);
                     }
                 }
-                __syncwarp();
             }
-            if (boxed != 0xffffffffu) {
-                // the others through registers, missing rows as zeros (a weight of zero does not undo what lay there)
-                constexpr int V = C::kRow / 16, kAhead = V % 4 == 0 ? 4 : 3;               // vectors of a row; of keys and of values in flight
-                const int64_t mine = ok ? (int64_t)r.id * a.c.stride_page + (int64_t)r.in * a.c.stride_token + r.head * a.c.stride_head : -1;
-                for (int x0 = 0; x0 < kAttTile * V; x0 += 32 * kAhead) {
-                    uint4 kx[kAhead], vx[kAhead];
-#pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        const int x = x0 + 32 * u + lane, line = x / V, v = x - line * V;
-                        const int64_t at = __shfl_sync(0xffffffffu, mine, line);
-                        kx[u] = vx[u] = make_uint4(0, 0, 0, 0);
-                        if (at >= 0 && !(boxed >> line & 1)) kx[u] = ld_once_u4(a.c.k + at + v * 16), vx[u] = ld_once_u4(a.c.v + at + v * 16);
-                    }
-#pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        const int x = x0 + 32 * u + lane, line = x / V, v = x - line * V;
-                        if (boxed >> line & 1) continue;
-                        uint8_t* to = tile + C::place(line, v);
-                        *reinterpret_cast<uint4*>(to) = kx[u];
-                        *reinterpret_cast<uint4*>(to + C::kHalf) = vx[u];
-                    }
-                }
-                fence_async();                                   // (the place's next tile may come by tensor copies)
-            }
-            if (F8)
-                *reinterpret_cast<float4*>(note + 16 * lane) =
-                    make_float4(kv_two_to(r.ke), ok ? 0.0f : -INFINITY, (float)min(max((int)r.ve - 127, -100), 112), ok ? kv_two_to(r.ve) : 0.0f);
-            else
-                *reinterpret_cast<float*>(note + 4 * lane) = ok ? 0.0f : -INFINITY;
-            if (r.flags & kAttTree) *reinterpret_cast<unsigned long long*>(note + C::kMasks + 8 * lane) = r.mask;
+            __syncwarp();
+            dirty &= ~(1ull << at);
         }
-        if (lane == 0) *reinterpret_cast<volatile uint32_t*>(note + C::kHeader) = (uint32_t)r.flags | (r.some ? 0u : (uint32_t)kAttEmpty);
+        if (boxed == 0xffffffffu) return;
+        // the others row by row, missing ones as zeros (a weight of zero does not undo what lay there)
+        dirty |= 1ull << at;
+        constexpr int V = C::kRow / 16;                          // vectors of a row
+        const int64_t mine = id >= 0 ? (int64_t)id * a.c.stride_page + (int64_t)in * a.c.stride_token + r.head * a.c.stride_head : -1;
+#pragma unroll 4
+        for (int x = lane; x < kAttTile * V; x += 32) {
+            const int line = x / V, v = x - line * V;
+            const int64_t from = __shfl_sync(0xffffffffu, mine, line);
+            if (boxed >> line & 1) continue;
+            const uint32_t to = tile + C::place(line, v);
+            cp16(to, a.c.k + (from >= 0 ? from + v * 16 : 0), from >= 0);
+            cp16(to + C::kHalf, a.c.v + (from >= 0 ? from + v * 16 : 0), from >= 0);
+        }
+    }
+
+    __device__ void note(const AttTokens& r, int turn, uint32_t at, bool some) {
+        if (some) {
+            const bool ok = r.id[turn] >= 0;
+            const uint32_t bias = ok ? 0u : 0xff800000u;
+            if (F8) {
+                const float ve = (float)min(max((int)r.ve[turn] - 127, -100), 112);
+                st_shared(at + 16 * lane, make_uint4(__float_as_uint(kv_two_to(r.ke[turn])), bias, __float_as_uint(ve), ok ? __float_as_uint(kv_two_to(r.ve[turn])) : 0u));
+            } else {
+                st_shared(at + 4 * lane, bias);
+            }
+            if (r.tree) {
+                st_shared(at + C::kMasks + 8 * lane, (uint32_t)r.mask[turn]);
+                st_shared(at + C::kMasks + 8 * lane + 4, (uint32_t)(r.mask[turn] >> 32));
+            }
+        }
+        // (a team's last tile of a round is the one of the highest number)
+        const bool end = r.last && kAttFeeds * turn + feed >= kAttFeeds * kAttTurns - C::kTeams;
+        if (lane == 0) st_shared(at + C::kHeader, (uint32_t)((end ? kAttEnd : 0) | (some ? 0 : kAttEmpty) | (r.tree ? kAttTree : 0)));
         __syncwarp();
-        if (lane == 0) mbar_arrive(full + place);
-        ++filled;
-        if (++place == C::kPer) place = 0, parity ^= 1;
     }
 
     __device__ void run() {
-        AttToken now, next, later;                               // exponents are asked for a round, page ids two rounds ahead of the copies
+        // e4m3: the exponents arrive while all of a round's copies are asked for (in a short ring that would hold a tile back for the next one's place)
+        constexpr bool kLate = F8 && C::kPer >= 2 * kAttTurns;
+        AttTokens now, next;                                     // page ids are asked for a round, exponents a round's copies ahead
         look_up(now);
-        resolve(now);
-        next.have = false;
-        if (now.have) look_up(next);
         while (now.have) {
-            if (next.have) resolve(next);
-            later.have = false;
-            if (next.have) look_up(later);
-            emit(now);
+            resolve(now);
+            look_up(next);
+            int at = place;
+            uint32_t p = parity;
+#pragma unroll
+            for (int t = 0; t < kAttTurns; ++t) {
+                att_wait(empty + 8 * at, p, dead, a.ctrl);
+                if (kAttTile * (kAttFeeds * t + feed) < now.n) copy(now, t, at);
+                if (!kLate) finish(now, t);
+                if (++at == C::kPer) at = 0, p ^= 1;
+            }
+#pragma unroll
+            for (int t = 0; t < (kLate ? kAttTurns : 0); ++t) finish(now, t);
             now = next;
-            next = later;
         }
         // No copy is in flight when the CTA ends, also when a wait has run out: the last use of every place in the ring lands.
         for (int k = max(0, filled - C::kPer); k < filled; ++k) {
             const unsigned long long t0 = global_ns();
-            while (!mbar_try(full + k % C::kPer, k / C::kPer & 1) && global_ns() - t0 < kAttWaitNs) {}
+            while (!bar_try(full + 8 * (k % C::kPer), k / C::kPer & 1) && global_ns() - t0 < kAttWaitNs) {}
         }
+    }
+    __device__ __forceinline__ void finish(const AttTokens& r, int t) {
+        note(r, t, notes + place * C::kNote, kAttTile * (kAttFeeds * t + feed) < r.n);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * place) : "memory");
+        if (lane == 0) bar_arrive(full + 8 * place);
+        ++filled;
+        if (++place == C::kPer) place = 0, parity ^= 1;
     }
 };
 
@@ -679,9 +709,8 @@ struct AttQueries {
     __device__ __forceinline__ void settle(float scale_log2, float (&scale)[2], uint8_t* qs, float* s_qscale, int warp, int lane) {
         scale[0] = scale[1] = scale_log2;
         if constexpr (C::kQRegs) {
-            if (!F8) return;
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
+            for (int r = 0; r < (F8 ? 2 : 0); ++r) {
                 uint32_t top = 0;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
@@ -741,6 +770,9 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     __shared__ long long s_sum[kAttWarps + kAttFeeds];
     __shared__ long long s_at[2], s_u[2];
     __shared__ int s_seq[2], s_dead;
+    __shared__ AttWalk s_walk[kAttWarps];
+    __shared__ AttSegment s_segment[kAttWarps];
+    __shared__ long long s_first[kAttWarps];
     uint8_t* notes = ring + C::kSlots * C::kSlot;
     uint8_t* qs = notes + C::kSlots * C::kNote;
     float4* meet = reinterpret_cast<float4*>(qs + C::kQBytes);
@@ -748,7 +780,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     int* lens = reinterpret_cast<int*>(parents + kKvMaxNodes);   // of the first kAttLens sequences
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid < C::kSlots) {
-        mbar_init(s_full + tid, 1);                              // the producer's word that all but its copies is there
+        mbar_init(s_full + tid, 33);                             // the producer's lanes, by their copies, and its word that the rest is there
         mbar_init(s_empty + tid, WR);
     }
     if (tid == 0) s_dead = 0;
@@ -819,8 +851,9 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     if (warp >= kAttWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAttProducerRegs));
         const int feed = warp - kAttWarps;
-        AttProducer<D, F8, WR> p{a, &k_map, &v_map, ring + feed * C::kPer * C::kSlot, notes + feed * C::kPer * C::kNote, s_full + feed * C::kPer,
-                                 s_empty + feed * C::kPer, parents, &s_dead, lens, walk, {}, groups, lane, feed, 0, false, -1, -1, -1, -1, -1};
+        AttProducer<D, F8, WR> p{a, &k_map, &v_map, smem_u32(ring) + feed * C::kPer * C::kSlot, smem_u32(notes) + feed * C::kPer * C::kNote,
+                                 smem_u32(s_full + feed * C::kPer), smem_u32(s_empty + feed * C::kPer), smem_u32(&s_dead), parents, lens, walk, {},
+                                 groups, lane, feed, 0, -1, -1, -1, -1, -1};
         p.run();
         return;
     }
@@ -828,18 +861,17 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
 
     const int team = warp / WR, wr = warp % WR, j = lane & 3;
     int4 meta = make_int4(-1, 0, 0, 0);
-    // the team's next tile: its producer, and its place there.  Eight teams: two to a producer, in turn; two: two producers each, in turn.
+    // the team's next tile: its producer, and its place there (two teams take those of two producers each, in turn)
     int feed = team % kAttFeeds, place = team / kAttFeeds;
     uint32_t parity = 0;
-    AttSegment g, after;
+    // (where the warp is in its run lies in shared memory while tiles are at work: the registers are theirs)
+    AttSegment g;
     AttQueries<D, F8, WR> q;
-    long long at = walk.u;
+    s_first[warp] = walk.u;
     att_next(a, lens, groups, walk, g);
+    s_segment[warp] = g, s_walk[warp] = walk;
     q.fetch(a, g, warp, lane);
-    for (bool go_on = true; go_on; g = after) {
-        const int row0 = g.group * 16 * WR;
-        const int r0 = row0 + wr * 16 + (lane >> 2), r1 = r0 + 8;
-        const int qi0 = min(r0, rows - 1) / a.group, qi1 = min(r1, rows - 1) / a.group;
+    for (bool go_on = true; go_on;) {
         float scale[2];
         q.settle(a.scale_log2, scale, qs, s_qscale, warp, lane);
         const uint32_t q_smem = smem_u32(qs) + wr * 16 * C::kQPitch;
@@ -848,28 +880,41 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         acc.clear();
         for (bool more = true; more;) {
             const int slot = feed * C::kPer + place;
-            att_wait(s_full + slot, parity, &s_dead, a.ctrl);
+            att_wait(smem_u32(s_full) + 8 * slot, parity, smem_u32(&s_dead), a.ctrl);
             uint8_t* tile = ring + slot * C::kSlot;
             const uint8_t* note = notes + slot * C::kNote;
-            const uint32_t header = *reinterpret_cast<const volatile uint32_t*>(note + C::kHeader);
+            const uint32_t header = ld_shared(smem_u32(note) + C::kHeader);
             if (!(header & kAttEmpty)) {
-                if (header & kAttTree) att_tile<D, F8, WR, true>(acc, q.f, q_smem, tile, note, scale, qi0, qi1);
-                else att_tile<D, F8, WR, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
+                if (header & kAttTree) {
+                    const int row = s_segment[warp].group * 16 * WR + wr * 16 + (lane >> 2);
+                    att_tile<D, F8, WR, true>(acc, q.f, q_smem, tile, note, scale, min(row, rows - 1) / a.group, min(row + 8, rows - 1) / a.group);
+                } else {
+                    att_tile<D, F8, WR, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
+                }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(s_empty + slot);
+            if (lane == 0) bar_arrive(smem_u32(s_empty) + 8 * slot);
             if (WR == 4) feed ^= 2;
             if (WR < 4 || feed < 2) {
                 place += C::kShare;
                 if (place >= C::kPer) place -= C::kPer, parity ^= 1;
             }
-            more = !(header & kAttEnd) && !*const_cast<volatile int*>(&s_dead);
+            more = !(header & kAttEnd) && !ld_shared(smem_u32(&s_dead));
         }
 
-        const long long at_next = walk.u;
-        go_on = att_next(a, lens, groups, walk, after);
-        if (go_on) q.fetch(a, after, warp, lane);                // (on their way while the results meet)
-        if (WR == 4) feed = team;
+        g = s_segment[warp];
+        const long long at = s_first[warp];
+        __syncwarp();
+        {
+            AttSegment after;
+            walk = s_walk[warp];
+            __syncwarp();
+            s_first[warp] = walk.u;
+            go_on = att_next(a, lens, groups, walk, after);
+            s_segment[warp] = after, s_walk[warp] = walk;
+            if (go_on) q.fetch(a, after, warp, lane);            // (on their way while the results meet)
+        }
+        const int row0 = g.group * 16 * WR, r0 = row0 + wr * 16 + (lane >> 2), r1 = r0 + 8;
 
         // the teams' parts meet, the upper half's with the lower half's: a lane hands its share to the lane with the same rows and dims
         consumers_barrier();                                     // (the meeting place is free)
@@ -908,9 +953,8 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         const bool whole = g.count == g.units;
         if (!whole && g.tile0 == 0)                              // the last CTA whose run begins within this result
             meta = make_int4((int)(((at + g.units - kAttSnap) * ctas - 1) / total), g.seq, g.head, g.group);
-        at = at_next;
         if (team != 0) continue;
-        const bool broken = *const_cast<volatile int*>(&s_dead) != 0;
+        const bool broken = ld_shared(smem_u32(&s_dead)) != 0;
         float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * (D + 2);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -918,7 +962,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             l += __shfl_xor_sync(0xffffffffu, l, 1);
             l += __shfl_xor_sync(0xffffffffu, l, 2);
             float m = acc.m[r];
-            const int row = r ? r1 : r0, qi = r ? qi1 : qi0;
+            const int row = r ? r1 : r0, qi = row / a.group;
             if (row >= rows) continue;
             const int64_t t = (int64_t)g.seq * a.Q + qi, to = t * a.Hq + g.head * a.group + (row - qi * a.group);
             const bool blind = a.node && ld_cg_s32(a.node + t) < -1;                       // a row of no token
