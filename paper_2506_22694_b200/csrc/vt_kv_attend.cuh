@@ -38,7 +38,8 @@ constexpr int kAttConsumerRegs = 200, kAttProducerRegs = 104;
 static_assert(kAttWarps * kAttConsumerRegs + kAttFeeds * kAttProducerRegs <= (kAttWarps + kAttFeeds) * 168, "what the block was launched with");
 constexpr int kAttUnit = 64;                                     // tokens
 // What a result counts for besides its tokens when the work is dealt out (the walk to it, its queries, the meeting), and a tree's tokens.
-constexpr int kAttPairUnits = 2, kAttTreeUnits = 2;
+// 64 ragged sequences of up to 8000 tokens, us with 2 / 4 / 8 / 12 for a result: bf16 186 / 174 / 169 / 170, e4m3 145 / 133 / 115 / 112.
+constexpr int kAttPairUnits = 8, kAttTreeUnits = 12;
 constexpr int kAttSnap = 2;                                      // no result is split so near to its ends
 constexpr int kAttLens = 1024;                                   // sequences whose lengths are kept in shared memory
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it

@@ -45,10 +45,20 @@ __device__ __forceinline__ uint32_t ld_cg_u8(const uint8_t* p) {
 }
 
 // ---- the row's arithmetic, in float or (keys that are rounded to 8 bits) in double ---------------------------------
-// A lane holds eight neighbouring dims of its head's row, LG lanes hold a row.
+// LG lanes hold a head's row, a lane two groups of four neighbouring dims.  They are the partners of each other's rotation: dims i and i + rot/2
+// (dims behind the rotated ones and interleaved pairs: two neighbouring groups), so that a lane makes four sines a token and hands nothing over.
+struct Groups {
+    int a, b;                     // first dims of the two
+    int angle;                    // frequency of the first pair, or -1: no rotation
+};
+__device__ __forceinline__ Groups groups_of(int sub, int rot, int interleaved) {
+    if (interleaved || 8 * sub >= rot) return {8 * sub, 8 * sub + 4, interleaved && 8 * sub < rot ? 4 * sub : -1};
+    return {4 * sub, 4 * sub + (rot >> 1), 4 * sub};
+}
+
 template <class F>
-struct Turn {                     // cosines and sines of a lane's eight dims
-    F c[8], s[8];
+struct Turn {                     // cosines and sines of a lane's four pairs
+    F c[4], s[4];
 };
 
 __device__ __forceinline__ void sin_cos_turns(int64_t turns, float& s, float& c) {        // turns: in units of 2^-64
@@ -59,44 +69,23 @@ __device__ __forceinline__ void sin_cos_turns(int64_t turns, double& s, double& 
 // Position times frequency is taken modulo one turn in whole numbers (64 bits of a turn, wrapping multiplication), which loses nothing at
 // any position; a product in fp32 is off by 0.004 rad at position 100000.
 template <class F>
-__device__ __forceinline__ void make_turn(Turn<F>& t, const int64_t* freqs, int rot, int interleaved, int dim, int32_t pos) {
+__device__ __forceinline__ void make_turn(Turn<F>& t, const int64_t* freqs, int angle, int32_t pos) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t.c[i] = F(1), t.s[i] = F(0);
-    if (!freqs || dim >= rot) return;
-    if (interleaved) {
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            F s, c;
-            sin_cos_turns((int64_t)((uint64_t)freqs[(dim + i) >> 1] * (uint64_t)(int64_t)pos), s, c);
-            t.c[i] = t.c[i + 1] = c, t.s[i] = -s, t.s[i + 1] = s;
-        }
-        return;
-    }
-    const int half = rot >> 1;
-    const bool low = dim < half;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        F s, c;
-        sin_cos_turns((int64_t)((uint64_t)freqs[(low ? dim : dim - half) + i] * (uint64_t)(int64_t)pos), s, c);
-        t.c[i] = c, t.s[i] = low ? -s : s;
+    for (int i = 0; i < 4; ++i) {
+        t.c[i] = F(1), t.s[i] = F(0);
+        if (angle >= 0) sin_cos_turns((int64_t)((uint64_t)freqs[angle + i] * (uint64_t)(int64_t)pos), t.s[i], t.c[i]);
     }
 }
 
-template <int LG>
-__device__ __forceinline__ float group_sum(float x) {
-#pragma unroll
-    for (int o = LG / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
-template <int LG>
-__device__ __forceinline__ double group_sum(double x) {
+template <int LG, class F>
+__device__ __forceinline__ F group_sum(F x) {
 #pragma unroll
     for (int o = LG / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
 
 template <int LG, class F>
-__device__ __forceinline__ void norm_rotate(F* x, const uint4& w, bool normed, double eps, int d, const Turn<F>& t, int rot, int interleaved, int dim) {
+__device__ __forceinline__ void norm_rotate(F* x, const uint4& w, bool normed, double eps, int d, const Turn<F>& t, int angle, int interleaved) {
     if (normed) {
         F sum = F(0);
 #pragma unroll
@@ -108,20 +97,13 @@ __device__ __forceinline__ void norm_rotate(F* x, const uint4& w, bool normed, d
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = x[i] * r * F(wf[i]);
     }
-    if (!rot) return;                                            // (uniform: no rotation at all)
-    F y[8];
-    if (interleaved) {
+    if (angle < 0) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-    } else {
-        const int lane = threadIdx.x & 31, step = rot >> 4;      // lanes between the partners of a pair
-        const int from = dim < (rot >> 1) ? lane + step : lane - step;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], from & 31);
-    }
-    if (dim < rot) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * t.c[i] + y[i] * t.s[i];
+    for (int i = 0; i < 4; ++i) {
+        F &a = interleaved ? x[2 * i] : x[i], &b = interleaved ? x[2 * i + 1] : x[4 + i];
+        const F y = a * t.c[i] - b * t.s[i];
+        b = b * t.c[i] + a * t.s[i];
+        a = y;
     }
 }
 
@@ -164,52 +146,64 @@ __device__ __forceinline__ uint2 to_e4m3(const F* x, uint32_t& exp_byte) {
 // ---- write ------------------------------------------------------------------------------------------------------
 // A warp takes a share of one token's heads, 32 / LG heads at a time, queries first, then keys, then values: the token's sines are made
 // once for all of them.  HBM-bound for prompts, latency-bound for a token; `shares` spreads a few tokens over more warps.
-template <int LG, bool E4M3>
-__global__ void __launch_bounds__(kThreads)
+template <int LG, bool E4M3, bool INTER>
+__global__ void __launch_bounds__(kThreads, E4M3 ? 3 : 4)
 k_qkv_write(const __grid_constant__ KvWriteArgs a, int shares) {
     griddep_launch_dependents();
     griddep_wait();
     constexpr int HP = 32 / LG;                                  // heads of a pass
-    const int lane = threadIdx.x & 31, sub = lane % LG, hl = lane / LG, dim = sub * 8, d = a.c.d;
-    const bool live = dim < d;
+    constexpr int kAhead = 4;                                    // passes of queries in flight
+    const int lane = threadIdx.x & 31, sub = lane % LG, hl = lane / LG, d = a.c.d;
+    const bool live = 8 * sub < d;
+    const Groups g = groups_of(sub, a.rot, INTER);
     const int q_passes = (a.Hq + HP - 1) / HP, k_passes = (a.c.heads + HP - 1) / HP, passes = q_passes + 2 * k_passes;
     const int64_t warps = (int64_t)gridDim.x * kWarps, all = (int64_t)a.T * shares;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    const uint4 wq = a.q_weight && live ? ld_cg_u4(a.q_weight + dim) : zero, wk = a.k_weight && live ? ld_cg_u4(a.k_weight + dim) : zero;
+    auto load = [&](const uint16_t* row, bool here) {
+        if (!here) return make_uint4(0, 0, 0, 0);
+        const uint2 lo = ld_once_u2(row + g.a), hi = ld_once_u2(row + g.b);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    };
+    auto store = [&](uint16_t* row, const uint4& x) {
+        *reinterpret_cast<uint2*>(row + g.a) = make_uint2(x.x, x.y);
+        *reinterpret_cast<uint2*>(row + g.b) = make_uint2(x.z, x.w);
+    };
+    auto store8 = [&](uint8_t* row, const uint2& x) {
+        *reinterpret_cast<uint32_t*>(row + g.a) = x.x;
+        *reinterpret_cast<uint32_t*>(row + g.b) = x.y;
+    };
+    const uint4 wq = load(a.q_weight, a.q_weight && live), wk = load(a.k_weight, a.k_weight && live);
     for (int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); item < all; item += warps) {
         const int64_t t = item / shares;
         const int share = (int)(item - t * shares);
         const int p0 = (int)((int64_t)passes * share / shares), p1 = (int)((int64_t)passes * (share + 1) / shares);
+        const int q_end = min(p1, q_passes), k_end = min(p1, q_passes + k_passes);
         const int32_t pos = a.freqs ? ld_cg_s32(a.positions + t) : 0;
         int64_t at = 0, exp_at = 0;
-        bool store = false;
+        bool place = false;
         if (p1 > q_passes) {
             const int32_t index = ld_cg_s32(a.index + t);
             if (index >= 0) {
-                store = kv_place(a.c, a.seq ? (int64_t)ld_cg_s32(a.seq + t) : t / (a.T / a.c.S), index, at, exp_at);
-                if (!store && lane == 0) kv_flag(a.ctrl);
+                place = kv_place(a.c, a.seq ? (int64_t)ld_cg_s32(a.seq + t) : t / (a.T / a.c.S), index, at, exp_at);
+                if (!place && lane == 0) kv_flag(a.ctrl);
             }
         }
-        const int q_end = min(p1, q_passes), k_end = min(p1, q_passes + k_passes);
         int p = p0;
         if (p < (E4M3 ? q_end : k_end)) {
             Turn<float> turn;
-            make_turn(turn, a.freqs, a.rot, a.interleaved, dim, pos);
-            for (; p < q_end; p += 4) {                          // queries, four passes in flight
-                uint4 raw[4];
+            uint4 raw[kAhead];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int h = (p + u) * HP + hl;
-                    raw[u] = live && p + u < q_end && h < a.Hq ? ld_once_u4(a.q + t * a.q_ld + (int64_t)h * d + dim) : zero;
-                }
+            for (int u = 0; u < kAhead; ++u) raw[u] = load(a.q + t * a.q_ld + (int64_t)((p + u) * HP + hl) * d, live && p + u < q_end && (p + u) * HP + hl < a.Hq);
+            make_turn(turn, a.freqs, a.freqs ? g.angle : -1, pos);                         // (while the first rows are on their way)
+            for (; p < q_end; p += kAhead) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+                for (int u = 0; u < kAhead; ++u) {
                     if (p + u >= q_end) break;
-                    const int h = (p + u) * HP + hl;
+                    const int h = (p + u) * HP + hl, next = h + kAhead * HP;
                     float x[8];
                     unpack8(raw[u], x);
-                    norm_rotate<LG>(x, wq, a.q_weight != nullptr, a.eps, d, turn, a.rot, a.interleaved, dim);
-                    if (live && h < a.Hq) *reinterpret_cast<uint4*>(a.q_out + (t * a.Hq + h) * d + dim) = pack8(x);
+                    raw[u] = load(a.q + t * a.q_ld + (int64_t)next * d, live && p + u + kAhead < q_end && next < a.Hq);
+                    norm_rotate<LG>(x, wq, a.q_weight != nullptr, a.eps, d, turn, g.angle, INTER);
+                    if (live && h < a.Hq) store(a.q_out + (t * a.Hq + h) * d, pack8(x));
                 }
             }
             p = max(p0, q_end);
@@ -217,29 +211,29 @@ k_qkv_write(const __grid_constant__ KvWriteArgs a, int shares) {
                 const int h = (p - q_passes) * HP + hl;
                 const bool here = live && h < a.c.heads;
                 float x[8];
-                unpack8(here ? ld_once_u4(a.k + t * a.k_ld + (int64_t)h * d + dim) : zero, x);
-                norm_rotate<LG>(x, wk, a.k_weight != nullptr, a.eps, d, turn, a.rot, a.interleaved, dim);
-                if (here && store) *reinterpret_cast<uint4*>(a.c.k + at + h * a.c.stride_head + 2 * dim) = pack8(x);
+                unpack8(load(a.k + t * a.k_ld + (int64_t)h * d, here), x);
+                norm_rotate<LG>(x, wk, a.k_weight != nullptr, a.eps, d, turn, g.angle, INTER);
+                if (here && place) store(reinterpret_cast<uint16_t*>(a.c.k + at + h * a.c.stride_head), pack8(x));
             }
         }
         if (E4M3 && p < k_end) {
             // Keys that are rounded to 8 bits are computed in 64: a key next to a border between two e4m3 values then falls to the right
             // side, so that the cache's bytes do not depend on the order of sums.
             Turn<double> turn;
-            make_turn(turn, a.freqs, a.rot, a.interleaved, dim, pos);
+            make_turn(turn, a.freqs, a.freqs ? g.angle : -1, pos);
             for (; p < k_end; ++p) {
                 const int h = (p - q_passes) * HP + hl;
                 const bool here = live && h < a.c.heads;
                 float f[8];
                 double x[8];
-                unpack8(here ? ld_once_u4(a.k + t * a.k_ld + (int64_t)h * d + dim) : zero, f);
+                unpack8(load(a.k + t * a.k_ld + (int64_t)h * d, here), f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = f[i];
-                norm_rotate<LG>(x, wk, a.k_weight != nullptr, a.eps, d, turn, a.rot, a.interleaved, dim);
+                norm_rotate<LG>(x, wk, a.k_weight != nullptr, a.eps, d, turn, g.angle, INTER);
                 uint32_t e;
                 const uint2 w = to_e4m3<LG>(x, e);
-                if (here && store) {
-                    *reinterpret_cast<uint2*>(a.c.k + at + h * a.c.stride_head + dim) = w;
+                if (here && place) {
+                    store8(a.c.k + at + h * a.c.stride_head, w);
                     if (sub == 0) a.c.k_exp[exp_at + (int64_t)h * a.c.page] = (uint8_t)e;
                 }
             }
@@ -247,17 +241,17 @@ k_qkv_write(const __grid_constant__ KvWriteArgs a, int shares) {
         for (; p < p1; ++p) {                                    // values
             const int h = (p - q_passes - k_passes) * HP + hl;
             const bool here = live && h < a.c.heads;
-            const uint4 raw = here ? ld_once_u4(a.v + t * a.v_ld + (int64_t)h * d + dim) : zero;
+            const uint4 raw = load(a.v + t * a.v_ld + (int64_t)h * d, here);
             if (!E4M3) {
-                if (here && store) *reinterpret_cast<uint4*>(a.c.v + at + h * a.c.stride_head + 2 * dim) = raw;
+                if (here && place) store(reinterpret_cast<uint16_t*>(a.c.v + at + h * a.c.stride_head), raw);
                 continue;
             }
             float x[8];
             unpack8(raw, x);
             uint32_t e;
             const uint2 w = to_e4m3<LG>(x, e);
-            if (here && store) {
-                *reinterpret_cast<uint2*>(a.c.v + at + h * a.c.stride_head + dim) = w;
+            if (here && place) {
+                store8(a.c.v + at + h * a.c.stride_head, w);
                 if (sub == 0) a.c.v_exp[exp_at + (int64_t)h * a.c.page] = (uint8_t)e;
             }
         }
@@ -394,13 +388,15 @@ struct Write {
     static cudaError_t go(const KvWriteArgs& a, cudaStream_t s) {
         constexpr int HP = 32 / LG;
         const int passes = (a.Hq + HP - 1) / HP + 2 * ((a.c.heads + HP - 1) / HP);
-        const int64_t seats = (int64_t)num_sms() * 2 * kWarps;   // two CTAs an SM: as many warps as its registers hold
+        const int64_t seats = (int64_t)num_sms() * 3 * kWarps;   // three CTAs an SM: about as many warps as its registers hold
         // few tokens: their heads are dealt to as many warps as there are seats, one pass each at the least
         int64_t shares = (2 * seats + a.T - 1) / a.T;
         if (shares > passes) shares = passes;
         const int64_t ctas = (a.T * shares + kWarps - 1) / kWarps;
-        const int64_t most = 4 * (int64_t)num_sms();
-        return launch_dependent(k_qkv_write<LG, E>, (unsigned)(ctas < most ? ctas : most), kThreads, 0, s, a, (int)shares);
+        const int64_t most = (E ? 3 : 4) * (int64_t)num_sms();
+        const unsigned grid = (unsigned)(ctas < most ? ctas : most);
+        if (a.interleaved) return launch_dependent(k_qkv_write<LG, E, true>, grid, kThreads, 0, s, a, (int)shares);
+        return launch_dependent(k_qkv_write<LG, E, false>, grid, kThreads, 0, s, a, (int)shares);
     }
 };
 template <int LG, bool E>
