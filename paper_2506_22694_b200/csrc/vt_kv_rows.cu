@@ -84,24 +84,89 @@ __device__ __forceinline__ F group_sum(F x) {
     return x;
 }
 
-template <int LG, class F>
-__device__ __forceinline__ void norm_rotate(F* x, const uint4& w, bool normed, double eps, int d, const Turn<F>& t, int angle, int interleaved) {
+// Two fp32 operations in one instruction: a prompt's rows are bound by the instructions that they take (4140 a token of 48 heads with
+// scalar operations and exact divisions: 60 us for 8.5k tokens).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 two(float lo, float hi) { return ((f2)__float_as_uint(hi) << 32) | __float_as_uint(lo); }
+__device__ __forceinline__ float lo_of(f2 x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float hi_of(f2 x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 y;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+    return y;
+}
+struct Turn2 {                    // a Turn in pairs, and the negative sines
+    f2 c[2], s[2], n[2];
+};
+__device__ __forceinline__ Turn2 in_pairs(const Turn<float>& t) {
+    Turn2 y;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        y.c[i] = two(t.c[2 * i], t.c[2 * i + 1]);
+        y.s[i] = two(t.s[2 * i], t.s[2 * i + 1]);
+        y.n[i] = two(-t.s[2 * i], -t.s[2 * i + 1]);
+    }
+    return y;
+}
+__device__ __forceinline__ void unpack_pairs(const uint4& v, f2* x) {
+    x[0] = two(bf_lo(v.x), bf_hi(v.x)), x[1] = two(bf_lo(v.y), bf_hi(v.y)), x[2] = two(bf_lo(v.z), bf_hi(v.z)), x[3] = two(bf_lo(v.w), bf_hi(v.w));
+}
+// A row of bf16 through norm and rotation, in fp32, back to bf16.  w: its weights in pairs; live: the lane holds a part of the row.
+template <int LG>
+__device__ __forceinline__ uint4 row_of_bf16(const uint4& raw, const f2* w, bool normed, float eps, float inv_d, bool live, const Turn2& t, bool turned, bool interleaved) {
+    f2 x[4];
+    unpack_pairs(raw, x);
     if (normed) {
-        F sum = F(0);
+        f2 sum = mul2(x[0], x[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) sum = fma2(x[i], x[i], sum);
+        const float r = rsqrtf(fmaf(group_sum<LG>(live ? lo_of(sum) + hi_of(sum) : 0.0f), inv_d, eps));
+        const f2 r2 = two(r, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = mul2(x[i], mul2(r2, w[i]));
+    }
+    if (turned && !interleaved) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f2 lo = x[i], hi = x[2 + i];
+            x[i] = fma2(hi, t.n[i], mul2(lo, t.c[i]));
+            x[2 + i] = fma2(lo, t.s[i], mul2(hi, t.c[i]));
+        }
+    } else if (turned) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float c = i & 1 ? hi_of(t.c[i >> 1]) : lo_of(t.c[i >> 1]), s = i & 1 ? hi_of(t.s[i >> 1]) : lo_of(t.s[i >> 1]);
+            const float lo = lo_of(x[i]), hi = hi_of(x[i]);
+            x[i] = two(lo * c - hi * s, hi * c + lo * s);
+        }
+    }
+    return make_uint4(bf_pack(lo_of(x[0]), hi_of(x[0])), bf_pack(lo_of(x[1]), hi_of(x[1])), bf_pack(lo_of(x[2]), hi_of(x[2])), bf_pack(lo_of(x[3]), hi_of(x[3])));
+}
+
+// The same of a row in 64 bits.
+template <int LG>
+__device__ __forceinline__ void norm_rotate(double* x, const uint4& w, bool normed, double eps, int d, const Turn<double>& t, int angle, bool interleaved) {
+    if (normed) {
+        double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
         sum = group_sum<LG>(sum);
-        const F r = F(1) / sqrt(sum / F(d) + F(eps));
+        const double r = 1.0 / sqrt(sum / (double)d + eps);
         float wf[8];
         unpack8(w, wf);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * F(wf[i]);
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (double)wf[i];
     }
     if (angle < 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        F &a = interleaved ? x[2 * i] : x[i], &b = interleaved ? x[2 * i + 1] : x[4 + i];
-        const F y = a * t.c[i] - b * t.s[i];
+        double &a = interleaved ? x[2 * i] : x[i], &b = interleaved ? x[2 * i + 1] : x[4 + i];
+        const double y = a * t.c[i] - b * t.s[i];
         b = b * t.c[i] + a * t.s[i];
         a = y;
     }
@@ -145,116 +210,148 @@ __device__ __forceinline__ uint2 to_e4m3(const F* x, uint32_t& exp_byte) {
 
 // ---- write ------------------------------------------------------------------------------------------------------
 // A warp takes a share of one token's heads, 32 / LG heads at a time, queries first, then keys, then values: the token's sines are made
-// once for all of them.  HBM-bound for prompts, latency-bound for a token; `shares` spreads a few tokens over more warps.
-template <int LG, bool E4M3, bool INTER>
-__global__ void __launch_bounds__(kThreads, E4M3 ? 3 : 4)
+// once for all of them.  For prompts bound by the memory and, close behind, by instructions (the head size is a constant for their sake);
+// latency-bound for a token: `shares` spreads a few tokens over more warps.
+template <int D>
+struct Rows {
+    static constexpr int kLanes = D <= 64 ? 8 : D <= 128 ? 16 : 32, kHeads = 32 / kLanes, kStep = kHeads * D;      // of a pass
+    static constexpr bool kAll = 8 * kLanes == D;                // no lane without a part of its row
+    const Groups g;
+    const int hl;
+    const bool live;
+
+    __device__ __forceinline__ uint4 load(const uint16_t* row) const {
+        const uint2 lo = ld_once_u2(row + g.a), hi = ld_once_u2(row + g.b);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+    __device__ __forceinline__ void store(uint16_t* row, const uint4& x) const {
+        *reinterpret_cast<uint2*>(row + g.a) = make_uint2(x.x, x.y);
+        *reinterpret_cast<uint2*>(row + g.b) = make_uint2(x.z, x.w);
+    }
+    __device__ __forceinline__ void store8(uint8_t* row, const uint2& x) const {
+        *reinterpret_cast<uint32_t*>(row + g.a) = x.x;
+        *reinterpret_cast<uint32_t*>(row + g.b) = x.y;
+    }
+    // passes [p, end) over a token's rows, N in flight: body(row, head, whether there is such a head for this lane)
+    template <int N, class Start, class Body>
+    __device__ __forceinline__ void passes(const uint16_t* rows, int heads, int p, int end, Start start, Body body) const {
+        bool begun = false;
+        for (; p < end; p += N) {
+            const uint16_t* from = rows + p * kStep + hl * D;
+            uint4 raw[N];
+            const bool full = p + N <= end && (p + N) * kHeads <= heads;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                raw[u] = make_uint4(0, 0, 0, 0);
+                if (full || (p + u < end && (p + u) * kHeads + hl < heads)) raw[u] = load(from + u * kStep);
+            }
+            if (!begun) start();                                 // (while the first rows are on their way)
+            begun = true;
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                if (full || p + u < end) body(raw[u], (p + u) * kHeads + hl, (kAll || live) && (full || (p + u) * kHeads + hl < heads));
+        }
+    }
+};
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(kThreads, 3)
 k_qkv_write(const __grid_constant__ KvWriteArgs a, int shares) {
     griddep_launch_dependents();
     griddep_wait();
-    constexpr int HP = 32 / LG;                                  // heads of a pass
-    constexpr int kAhead = 4;                                    // passes of queries in flight
-    const int lane = threadIdx.x & 31, sub = lane % LG, hl = lane / LG, d = a.c.d;
-    const bool live = 8 * sub < d;
-    const Groups g = groups_of(sub, a.rot, INTER);
+    using R = Rows<D>;
+    constexpr int LG = R::kLanes, HP = R::kHeads;
+    const int lane = threadIdx.x & 31, sub = lane % LG;
+    const bool live = 8 * sub < D, inter = a.interleaved;
+    // (a lane without a part of the row goes along with the first)
+    const R rows{live ? groups_of(sub, a.rot, a.interleaved) : Groups{0, 4, -1}, lane / LG, live};
+    const int angle = a.freqs ? rows.g.angle : -1;
     const int q_passes = (a.Hq + HP - 1) / HP, k_passes = (a.c.heads + HP - 1) / HP, passes = q_passes + 2 * k_passes;
     const int64_t warps = (int64_t)gridDim.x * kWarps, all = (int64_t)a.T * shares;
-    auto load = [&](const uint16_t* row, bool here) {
-        if (!here) return make_uint4(0, 0, 0, 0);
-        const uint2 lo = ld_once_u2(row + g.a), hi = ld_once_u2(row + g.b);
-        return make_uint4(lo.x, lo.y, hi.x, hi.y);
-    };
-    auto store = [&](uint16_t* row, const uint4& x) {
-        *reinterpret_cast<uint2*>(row + g.a) = make_uint2(x.x, x.y);
-        *reinterpret_cast<uint2*>(row + g.b) = make_uint2(x.z, x.w);
-    };
-    auto store8 = [&](uint8_t* row, const uint2& x) {
-        *reinterpret_cast<uint32_t*>(row + g.a) = x.x;
-        *reinterpret_cast<uint32_t*>(row + g.b) = x.y;
-    };
-    const uint4 wq = load(a.q_weight, a.q_weight && live), wk = load(a.k_weight, a.k_weight && live);
+    const bool q_normed = a.q_weight != nullptr, k_normed = a.k_weight != nullptr;
+    const uint4 none = make_uint4(0, 0, 0, 0), wq = q_normed ? rows.load(a.q_weight) : none, wk = k_normed ? rows.load(a.k_weight) : none;
+    const float eps = (float)a.eps, inv_d = 1.0f / (float)D;
     for (int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); item < all; item += warps) {
-        const int64_t t = item / shares;
+        const int64_t t = shares == 1 ? item : item / shares;
         const int share = (int)(item - t * shares);
-        const int p0 = (int)((int64_t)passes * share / shares), p1 = (int)((int64_t)passes * (share + 1) / shares);
-        const int q_end = min(p1, q_passes), k_end = min(p1, q_passes + k_passes);
+        const int p0 = passes * share / shares, p1 = passes * (share + 1) / shares;
+        const int q_end = min(p1, q_passes), k_begin = max(p0, q_passes), k_end = min(p1, q_passes + k_passes), v_begin = max(p0, q_passes + k_passes);
+        const bool keys = p1 > q_passes;
         const int32_t pos = a.freqs ? ld_cg_s32(a.positions + t) : 0;
+        const int32_t index = keys ? ld_cg_s32(a.index + t) : -1;
+        const int64_t seq = !keys ? 0 : a.seq ? (int64_t)ld_cg_s32(a.seq + t) : t / (a.T / a.c.S);
         int64_t at = 0, exp_at = 0;
-        bool place = false;
-        if (p1 > q_passes) {
-            const int32_t index = ld_cg_s32(a.index + t);
-            if (index >= 0) {
-                place = kv_place(a.c, a.seq ? (int64_t)ld_cg_s32(a.seq + t) : t / (a.T / a.c.S), index, at, exp_at);
-                if (!place && lane == 0) kv_flag(a.ctrl);
-            }
+        bool place = false, placed = false;
+        auto find = [&] {
+            if (placed) return;
+            placed = true;
+            if (index < 0) return;
+            place = kv_place(a.c, seq, index, at, exp_at);
+            if (!place && lane == 0) kv_flag(a.ctrl);
+        };
+        Turn2 turn;
+        bool turned = false;
+        auto sines = [&] {
+            if (turned) return;
+            turned = true;
+            Turn<float> angles;
+            make_turn(angles, a.freqs, angle, pos);
+            turn = in_pairs(angles);
+        };
+        if (p0 < q_end) {
+            uint16_t* out = a.q_out + t * a.Hq * D;
+            f2 w[4];
+            unpack_pairs(wq, w);
+            rows.template passes<4>(a.q + t * a.q_ld, a.Hq, p0, q_end, sines, [&](const uint4& row, int h, bool here) {
+                const uint4 y = row_of_bf16<LG>(row, w, q_normed, eps, inv_d, R::kAll || live, turn, angle >= 0, inter);
+                if (here) rows.store(out + h * D, y);
+            });
         }
-        int p = p0;
-        if (p < (E4M3 ? q_end : k_end)) {
-            Turn<float> turn;
-            uint4 raw[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) raw[u] = load(a.q + t * a.q_ld + (int64_t)((p + u) * HP + hl) * d, live && p + u < q_end && (p + u) * HP + hl < a.Hq);
-            make_turn(turn, a.freqs, a.freqs ? g.angle : -1, pos);                         // (while the first rows are on their way)
-            for (; p < q_end; p += kAhead) {
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    if (p + u >= q_end) break;
-                    const int h = (p + u) * HP + hl, next = h + kAhead * HP;
-                    float x[8];
-                    unpack8(raw[u], x);
-                    raw[u] = load(a.q + t * a.q_ld + (int64_t)next * d, live && p + u + kAhead < q_end && next < a.Hq);
-                    norm_rotate<LG>(x, wq, a.q_weight != nullptr, a.eps, d, turn, g.angle, INTER);
-                    if (live && h < a.Hq) store(a.q_out + (t * a.Hq + h) * d, pack8(x));
-                }
-            }
-            p = max(p0, q_end);
-            for (; !E4M3 && p < k_end; ++p) {                    // keys of a bf16 cache
-                const int h = (p - q_passes) * HP + hl;
-                const bool here = live && h < a.c.heads;
-                float x[8];
-                unpack8(load(a.k + t * a.k_ld + (int64_t)h * d, here), x);
-                norm_rotate<LG>(x, wk, a.k_weight != nullptr, a.eps, d, turn, g.angle, INTER);
-                if (here && place) store(reinterpret_cast<uint16_t*>(a.c.k + at + h * a.c.stride_head), pack8(x));
-            }
+        if (k_begin < k_end && !E4M3) {
+            f2 w[4];
+            unpack_pairs(wk, w);
+            rows.template passes<4>(a.k + t * a.k_ld, a.c.heads, k_begin - q_passes, k_end - q_passes, [&] { sines(); find(); }, [&](const uint4& row, int h, bool here) {
+                const uint4 y = row_of_bf16<LG>(row, w, k_normed, eps, inv_d, R::kAll || live, turn, angle >= 0, inter);
+                if (here && place) rows.store(reinterpret_cast<uint16_t*>(a.c.k + at + h * a.c.stride_head), y);
+            });
         }
-        if (E4M3 && p < k_end) {
+        if (k_begin < k_end && E4M3) {
             // Keys that are rounded to 8 bits are computed in 64: a key next to a border between two e4m3 values then falls to the right
             // side, so that the cache's bytes do not depend on the order of sums.
-            Turn<double> turn;
-            make_turn(turn, a.freqs, a.freqs ? g.angle : -1, pos);
-            for (; p < k_end; ++p) {
-                const int h = (p - q_passes) * HP + hl;
-                const bool here = live && h < a.c.heads;
+            Turn<double> exact;
+            rows.template passes<1>(a.k + t * a.k_ld, a.c.heads, k_begin - q_passes, k_end - q_passes, [&] { make_turn(exact, a.freqs, angle, pos); find(); },
+                                    [&](const uint4& row, int h, bool here) {
                 float f[8];
                 double x[8];
-                unpack8(load(a.k + t * a.k_ld + (int64_t)h * d, here), f);
+                unpack8(row, f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = f[i];
-                norm_rotate<LG>(x, wk, a.k_weight != nullptr, a.eps, d, turn, g.angle, INTER);
+                for (int i = 0; i < 8; ++i) x[i] = R::kAll || live ? f[i] : 0.0f;
+                norm_rotate<LG>(x, wk, k_normed, a.eps, D, exact, angle, inter);
                 uint32_t e;
-                const uint2 w = to_e4m3<LG>(x, e);
+                const uint2 y = to_e4m3<LG>(x, e);
                 if (here && place) {
-                    store8(a.c.k + at + h * a.c.stride_head, w);
+                    rows.store8(a.c.k + at + h * a.c.stride_head, y);
                     if (sub == 0) a.c.k_exp[exp_at + (int64_t)h * a.c.page] = (uint8_t)e;
                 }
-            }
+            });
         }
-        for (; p < p1; ++p) {                                    // values
-            const int h = (p - q_passes - k_passes) * HP + hl;
-            const bool here = live && h < a.c.heads;
-            const uint4 raw = load(a.v + t * a.v_ld + (int64_t)h * d, here);
-            if (!E4M3) {
-                if (here && place) store(reinterpret_cast<uint16_t*>(a.c.v + at + h * a.c.stride_head), raw);
-                continue;
-            }
-            float x[8];
-            unpack8(raw, x);
-            uint32_t e;
-            const uint2 w = to_e4m3<LG>(x, e);
-            if (here && place) {
-                store8(a.c.v + at + h * a.c.stride_head, w);
-                if (sub == 0) a.c.v_exp[exp_at + (int64_t)h * a.c.page] = (uint8_t)e;
-            }
-        }
+        if (v_begin < p1)
+            rows.template passes<4>(a.v + t * a.v_ld, a.c.heads, v_begin - q_passes - k_passes, p1 - q_passes - k_passes, find, [&](const uint4& row, int h, bool here) {
+                if (!E4M3) {
+                    if (here && place) rows.store(reinterpret_cast<uint16_t*>(a.c.v + at + h * a.c.stride_head), row);
+                    return;
+                }
+                float x[8];
+                unpack8(row, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = R::kAll || live ? x[i] : 0.0f;
+                uint32_t e;
+                const uint2 y = to_e4m3<LG>(x, e);
+                if (here && place) {
+                    rows.store8(a.c.v + at + h * a.c.stride_head, y);
+                    if (sub == 0) a.c.v_exp[exp_at + (int64_t)h * a.c.page] = (uint8_t)e;
+                }
+            });
     }
 }
 
@@ -374,6 +471,21 @@ k_kv_commit(const __grid_constant__ KvCommitArgs a) {
     }
 }
 
+template <int D>
+cudaError_t write_go(const KvWriteArgs& a, cudaStream_t s) {
+    constexpr int HP = Rows<D>::kHeads;
+    const int passes = (a.Hq + HP - 1) / HP + 2 * ((a.c.heads + HP - 1) / HP);
+    const int64_t most = 3 * (int64_t)num_sms();                 // three CTAs an SM: as many warps as its registers hold
+    // few tokens: their heads are dealt to as many warps as there are seats, one pass each at the least
+    int64_t shares = most * kWarps / a.T;
+    if (shares > passes) shares = passes;
+    if (shares < 1) shares = 1;
+    const int64_t ctas = (a.T * shares + kWarps - 1) / kWarps;
+    const unsigned grid = (unsigned)(ctas < most ? ctas : most);
+    if (a.c.k_exp) return launch_dependent(k_qkv_write<D, true>, grid, kThreads, 0, s, a, (int)shares);
+    return launch_dependent(k_qkv_write<D, false>, grid, kThreads, 0, s, a, (int)shares);
+}
+
 template <template <int, bool> class Run, class A>
 cudaError_t by_shape(const A& a, cudaStream_t s) {
     const bool e = a.c.k_exp != nullptr;
@@ -382,23 +494,6 @@ cudaError_t by_shape(const A& a, cudaStream_t s) {
     if (d <= 128) return e ? Run<16, true>::go(a, s) : Run<16, false>::go(a, s);
     return e ? Run<32, true>::go(a, s) : Run<32, false>::go(a, s);
 }
-
-template <int LG, bool E>
-struct Write {
-    static cudaError_t go(const KvWriteArgs& a, cudaStream_t s) {
-        constexpr int HP = 32 / LG;
-        const int passes = (a.Hq + HP - 1) / HP + 2 * ((a.c.heads + HP - 1) / HP);
-        const int64_t seats = (int64_t)num_sms() * 3 * kWarps;   // three CTAs an SM: about as many warps as its registers hold
-        // few tokens: their heads are dealt to as many warps as there are seats, one pass each at the least
-        int64_t shares = (2 * seats + a.T - 1) / a.T;
-        if (shares > passes) shares = passes;
-        const int64_t ctas = (a.T * shares + kWarps - 1) / kWarps;
-        const int64_t most = (E ? 3 : 4) * (int64_t)num_sms();
-        const unsigned grid = (unsigned)(ctas < most ? ctas : most);
-        if (a.interleaved) return launch_dependent(k_qkv_write<LG, E, true>, grid, kThreads, 0, s, a, (int)shares);
-        return launch_dependent(k_qkv_write<LG, E, false>, grid, kThreads, 0, s, a, (int)shares);
-    }
-};
 template <int LG, bool E>
 struct Read {
     static cudaError_t go(const KvReadArgs& a, cudaStream_t s) {
@@ -409,7 +504,16 @@ struct Read {
 
 }  // namespace
 
-cudaError_t launch_qkv_write(const KvWriteArgs& a, cudaStream_t s) { return a.T ? by_shape<Write>(a, s) : cudaSuccess; }
+cudaError_t launch_qkv_write(const KvWriteArgs& a, cudaStream_t s) {
+    if (!a.T) return cudaSuccess;
+    switch (a.c.d) {
+        case 64: return write_go<64>(a, s);
+        case 96: return write_go<96>(a, s);
+        case 128: return write_go<128>(a, s);
+        case 192: return write_go<192>(a, s);
+        default: return write_go<256>(a, s);
+    }
+}
 cudaError_t launch_kv_read(const KvReadArgs& a, cudaStream_t s) { return a.T ? by_shape<Read>(a, s) : cudaSuccess; }
 cudaError_t launch_kv_commit(const KvCommitArgs& a, cudaStream_t s) {
     return launch_dependent(k_kv_commit, (unsigned)a.c.S, kThreads, 0, s, a);
