@@ -219,12 +219,13 @@ struct AttAcc {
 };
 
 // One tile: scores of the warp's 16 rows with its tokens, running maximum, weighted values.  LIST: tokens are a tree's nodes, and the
-// tile's masks say which new rows see each.
-template <int D, bool F8, int WR, bool LIST>
+// tile's masks say which new rows see each.  HALF: there are eight rows at the most, the lanes' second rows are none.
+template <int D, bool F8, int WR, bool HALF, bool LIST>
 __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, uint8_t* slot, const uint8_t* note, const float (&scale)[2],
                                          int qi0, int qi1) {
     using C = AttCfg<D, F8, WR>;
     constexpr int NT = C::kTile / 8;                             // groups of 8 tokens
+    constexpr int NR = HALF ? 1 : 2;                             // rows of a lane
     const int lane = threadIdx.x & 31, j = lane & 3;
     float s[NT][4];
 #pragma unroll
@@ -277,12 +278,14 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
             float bias;
             if (F8) {
                 const float4 x = *reinterpret_cast<const float4*>(note + 16 * t);
-                s[i][u] *= x.x, s[i][2 + u] *= x.x;
+                s[i][u] *= x.x;
+                if (!HALF) s[i][2 + u] *= x.x;
                 bias = x.y, ve[u] = x.z, vf[i][u] = x.w;
             } else {
                 bias = *reinterpret_cast<const float*>(note + 4 * t);
             }
-            s[i][u] = fmaf(s[i][u], scale[0], bias), s[i][2 + u] = fmaf(s[i][2 + u], scale[1], bias);
+            s[i][u] = fmaf(s[i][u], scale[0], bias);
+            if (!HALF) s[i][2 + u] = fmaf(s[i][2 + u], scale[1], bias);
             if (LIST) {
                 const unsigned long long bits = *reinterpret_cast<const unsigned long long*>(note + C::kMasks + 8 * t);
                 const bool r0 = (bits >> qi0) & 1, r1 = (bits >> qi1) & 1;
@@ -290,12 +293,13 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                 if (!r0) s[i][u] = -INFINITY;
                 if (!r1) s[i][2 + u] = -INFINITY;
             }
-            top[0] = fmaxf(top[0], s[i][u] + ve[u]), top[1] = fmaxf(top[1], s[i][2 + u] + ve[u]);
+            top[0] = fmaxf(top[0], s[i][u] + ve[u]);
+            if (!HALF) top[1] = fmaxf(top[1], s[i][2 + u] + ve[u]);
         }
     }
     bool grows = false;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < NR; ++r) {
         top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
         top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
         grows |= top[r] > acc.m[r] + 4.0f;
@@ -304,7 +308,7 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
     // and most tiles need not scale what is there.
     if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < NR; ++r) {
             const float m = fmaxf(acc.m[r], top[r]);
             const float f = m == acc.m[r] ? 1.0f : exp2_fast(acc.m[r] - m);
             acc.m[r] = m;
@@ -317,11 +321,14 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
         s[i][0] = exp2_fast(s[i][0] - m0), s[i][1] = exp2_fast(s[i][1] - m0);
-        s[i][2] = exp2_fast(s[i][2] - m1), s[i][3] = exp2_fast(s[i][3] - m1);
         acc.l[0] += s[i][0] + s[i][1];
-        acc.l[1] += s[i][2] + s[i][3];
+        if (!HALF) {
+            s[i][2] = exp2_fast(s[i][2] - m1), s[i][3] = exp2_fast(s[i][3] - m1);
+            acc.l[1] += s[i][2] + s[i][3];
+        }
         if (F8) {
-            s[i][0] *= vf[i][0], s[i][1] *= vf[i][1], s[i][2] *= vf[i][0], s[i][3] *= vf[i][1];
+            s[i][0] *= vf[i][0], s[i][1] *= vf[i][1];
+            if (!HALF) s[i][2] *= vf[i][0], s[i][3] *= vf[i][1];
             if (LIST) {                                          // (a power of a row that held a NaN is one)
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -380,6 +387,8 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                            // i: (row half, token half) of the A fragment
+            hi[i] = lo[i] = 0;
+            if (HALF && (i & 1)) continue;
             const float x = s[2 * g + (i >> 1)][2 * (i & 1)], y = s[2 * g + (i >> 1)][2 * (i & 1) + 1];
             if (F8) {
                 const __half2 h = __floats2half2_rn(x, y);
@@ -760,7 +769,7 @@ struct AttQueries {
     }
 };
 
-template <int D, bool F8, int WR>
+template <int D, bool F8, int WR, bool HALF>
 __global__ void __launch_bounds__(kAttThreads, 1)
 k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     using C = AttCfg<D, F8, WR>;
@@ -888,9 +897,9 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             if (!(header & kAttEmpty)) {
                 if (header & kAttTree) {
                     const int row = s_segment[warp].group * 16 * WR + wr * 16 + (lane >> 2);
-                    att_tile<D, F8, WR, true>(acc, q.f, q_smem, tile, note, scale, min(row, rows - 1) / a.group, min(row + 8, rows - 1) / a.group);
+                    att_tile<D, F8, WR, HALF, true>(acc, q.f, q_smem, tile, note, scale, min(row, rows - 1) / a.group, min(row + 8, rows - 1) / a.group);
                 } else {
-                    att_tile<D, F8, WR, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
+                    att_tile<D, F8, WR, HALF, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
                 }
             }
             __syncwarp();
@@ -1007,7 +1016,7 @@ bool kv_map(CUtensorMap* map, const KvView& c, const uint8_t* base, bool f8, int
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool F8, int WR>
+template <int D, bool F8, int WR, bool HALF = false>
 cudaError_t attend_go(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
     using C = AttCfg<D, F8, WR>;
     static bool ready[64] = {false};                             // by device
@@ -1015,7 +1024,7 @@ cudaError_t attend_go(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    auto* kernel = k_kv_attend<D, F8, WR>;
+    auto* kernel = k_kv_attend<D, F8, WR, HALF>;
     if (!ready[dev]) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
         if (e != cudaSuccess) return e;
@@ -1051,6 +1060,7 @@ template <int D, bool F8>
 cudaError_t attend_rows(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
     const int wr = kv_attend_warp_rows(a.Q * a.group, D);
     if constexpr (D <= 128) {
+        if (a.Q * a.group <= 8) return attend_go<D, F8, 1, true>(a, ctas, s);
         if (wr == 1) return attend_go<D, F8, 1>(a, ctas, s);
         if (wr == 4) return attend_go<D, F8, 4>(a, ctas, s);
     }
