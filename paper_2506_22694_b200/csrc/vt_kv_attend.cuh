@@ -559,7 +559,8 @@ struct AttProducer {
                 r.id[t] = -2;
             }
             if (F8) {
-                const int64_t e = r.id[t] >= 0 ? ((int64_t)r.id[t] * a.c.heads + r.head) * a.c.page + r.in[t] : 0;
+                // (fewer than 2^31 rows fit any GPU's memory)
+                const uint32_t e = r.id[t] >= 0 ? ((uint32_t)r.id[t] * a.c.heads + r.head) * a.c.page + r.in[t] : 0u;
                 asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(r.ke[t]) : "l"(a.c.k_exp + e) : "memory");
                 asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(r.ve[t]) : "l"(a.c.v_exp + e) : "memory");
             }
@@ -567,18 +568,36 @@ struct AttProducer {
     }
 
     // A tile's rows.  16 or 32 tokens of a page at a time come by tensor copies, where they are all there.
-    __device__ void copy(const AttTokens& r, int turn, int at) {
+    __device__ __forceinline__ void copy(const AttTokens& r, int turn, int at) {
         const uint32_t tile = ring + at * C::kSlot, bar = full + 8 * at;
         const int32_t id = r.id[turn], in = r.in[turn];
-        const unsigned have = __ballot_sync(0xffffffffu, id >= 0);
+        const int rest = r.n - kAttTile * (kAttFeeds * turn + feed);                       // tokens of the tile, and of those behind it
         unsigned boxed = 0;                                      // tokens that come so
-        if (!r.tree && a.box == 32) boxed = have == 0xffffffffu ? have : 0u;
-        else if (!r.tree && a.box == 16) boxed = ((have & 0xffffu) == 0xffffu ? 0xffffu : 0u) | ((have >> 16) == 0xffffu ? 0xffff0000u : 0u);
-        if (boxed) {
+        if (!r.tree && a.box == 32 && rest >= 32) {
+            const int id0 = __shfl_sync(0xffffffffu, id, 0), in0 = __shfl_sync(0xffffffffu, in, 0);
+            if (id0 >= 0) {
+                boxed = 0xffffffffu;
+                if (elect_lane()) {
+                    if (dirty >> at & 1) fence_async();          // (what threads have stored there comes first)
+                    bar_expect(bar, 2 * 32 * C::kRow);
+#pragma unroll
+                    for (int x = 0; x < C::kRow / C::kBox; ++x) {
+                        const uint32_t to = tile + x * C::kTile * C::kBox;
+                        const int dim = x * (F8 ? C::kBox : C::kBox / 2);
+                        box_copy(to, k_map, dim, in0, r.head, id0, bar);
+                        box_copy(to + C::kHalf, v_map, dim, in0, r.head, id0, bar);
+                    }
+                }
+                __syncwarp();
+                dirty &= ~(1ull << at);
+                return;
+            }
+        } else if (!r.tree && a.box == 16 && rest >= 16) {
             const int id0 = __shfl_sync(0xffffffffu, id, 0), in0 = __shfl_sync(0xffffffffu, in, 0);
             const int id1 = __shfl_sync(0xffffffffu, id, 16), in1 = __shfl_sync(0xffffffffu, in, 16);
-            if (elect_lane()) {
-                if (dirty >> at & 1) fence_async();              // (what threads have stored there comes first)
+            boxed = (id0 >= 0 ? 0xffffu : 0u) | (id1 >= 0 && rest >= 32 ? 0xffff0000u : 0u);
+            if (boxed && elect_lane()) {
+                if (dirty >> at & 1) fence_async();
                 bar_expect(bar, __popc(boxed) * 2 * C::kRow);
 #pragma unroll
                 for (int x = 0; x < C::kRow / C::kBox; ++x) {
@@ -588,16 +607,16 @@ struct AttProducer {
                         box_copy(to, k_map, dim, in0, r.head, id0, bar);
                         box_copy(to + C::kHalf, v_map, dim, in0, r.head, id0, bar);
                     }
-                    if (a.box == 16 && (boxed >> 31)) {
+                    if (boxed >> 31) {
                         box_copy(to + 16 * C::kBox, k_map, dim, in1, r.head, id1, bar);
                         box_copy(to + C::kHalf + 16 * C::kBox, v_map, dim, in1, r.head, id1, bar);
                     }
                 }
             }
             __syncwarp();
-            dirty &= ~(1ull << at);
+            if (boxed) dirty &= ~(1ull << at);
+            if (boxed == 0xffffffffu) return;
         }
-        if (boxed == 0xffffffffu) return;
         // the others row by row, missing ones as zeros (a weight of zero does not undo what lay there)
         dirty |= 1ull << at;
         constexpr int V = C::kRow / 16;                          // vectors of a row
@@ -644,9 +663,13 @@ struct AttProducer {
             look_up(next);
             int at = place;
             uint32_t p = parity;
+            // (a look at a barrier takes 200 cycles: at both places' at once)
+            bool given[kAttTurns];
+#pragma unroll
+            for (int t = 0; t < kAttTurns; ++t) given[t] = bar_try(empty + 8 * ((place + t) % C::kPer), place + t >= C::kPer ? parity ^ 1 : parity);
 #pragma unroll
             for (int t = 0; t < kAttTurns; ++t) {
-                att_wait(empty + 8 * at, p, dead, a.ctrl);
+                if (!given[t] || C::kPer < kAttTurns) att_wait(empty + 8 * at, p, dead, a.ctrl);
                 if (kAttTile * (kAttFeeds * t + feed) < now.n) copy(now, t, at);
                 if (!kLate) finish(now, t);
                 if (++at == C::kPer) at = 0, p ^= 1;
