@@ -16,7 +16,8 @@ struct Ctrl {
     unsigned long long n_bad;     // ids skipped by the histogram
     unsigned long long wait_ns;   // bound of a device-side wait in nanoseconds (0 = the built-in default)
     uint32_t head_aborted;        // a CTA of the head kernel gave up on a wait: its call's merge reports and clears it
-    uint32_t pad[57];
+    uint32_t kv_tickets[40];      // paged attention: parts of a result that have arrived, a byte each (every result leaves its own at zero)
+    uint32_t pad[17];
 };
 static_assert(sizeof(Ctrl) == VT_CTRL_BYTES, "control block size");
 

@@ -73,6 +73,9 @@ struct KvAttendArgs {
     Ctrl* ctrl;
 };
 int kv_attend_warp_rows(int rows, int d);        // warps side by side over a key head's rows (1, 2 or 4 of 16 rows each)
+// Whether the attention kernel joins its parts itself: up to eight rows.  The CTA whose part arrives last reads them all, 40 KB for four rows and 19
+// parts; a kernel of its own, which deals more rows out to all CTAs, costs 2.5 us.
+inline bool kv_attend_joins(int rows, int d) { return rows <= 8 && d <= 128; }
 size_t kv_attend_scratch_bytes(int rows, int d);
 cudaError_t launch_kv_attend_bf16(const KvAttendArgs& a, int& ctas, cudaStream_t s);
 cudaError_t launch_kv_attend_e4m3(const KvAttendArgs& a, int& ctas, cudaStream_t s);

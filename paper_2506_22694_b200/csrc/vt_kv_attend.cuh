@@ -23,7 +23,7 @@
 #pragma once
 #include <cuda_fp16.h>
 
-#include "vt_kv.cuh"
+#include "vt_kv_join.cuh"
 #include "vt_maps.cuh"
 #include "vt_mbar.cuh"
 
@@ -421,6 +421,11 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
     }
 }
 
+// Quotients of numbers that nearly always fit 32 bits (a division of 64 takes some hundred instructions).
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+    return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 // The run of units of a CTA, segment by segment; the producer and the consumers walk it each on their own.
 struct AttWalk {
     long long u, u1, off;         // next unit, end, and the next unit's place in its sequence
@@ -443,7 +448,7 @@ __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens,
     g.seq = w.seq;
     g.len = g.seq < kAttLens ? lens[g.seq] : att_len(a, g.seq);
     g.units = att_units(a, g.len);
-    const int pair = (int)(w.off / g.units);
+    const int pair = (int)quotient(w.off, g.units);
     g.tile0 = (int)(w.off - (long long)pair * g.units);
     g.count = (int)min((long long)(g.units - g.tile0), w.u1 - w.u);
     g.head = pair / groups, g.group = pair - g.head * groups;
@@ -806,6 +811,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     __shared__ AttWalk s_walk[kAttWarps];
     __shared__ AttSegment s_segment[kAttWarps];
     __shared__ long long s_first[kAttWarps];
+    __shared__ int4 s_join[2];                                   // results that this CTA joins: first CTA, parts, sequence, head
     uint8_t* notes = ring + C::kSlots * C::kSlot;
     uint8_t* qs = notes + C::kSlots * C::kNote;
     float4* meet = reinterpret_cast<float4*>(qs + C::kQBytes);
@@ -816,7 +822,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         mbar_init(s_full + tid, 33);                             // the producer's lanes, by their copies, and its word that the rest is there
         mbar_init(s_empty + tid, WR);
     }
-    if (tid == 0) s_dead = 0;
+    if (tid == 0) s_dead = 0, s_join[0].x = s_join[1].x = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     griddep_launch_dependents();
     griddep_wait();
@@ -848,11 +854,13 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     before *= per_unit;
     mine *= per_unit;
     const long long ctas = min((long long)gridDim.x, total);
+    const long long each = quotient(total, ctas);
     // The run begins and ends where equal shares do, but not within a result's first or last units: a piece that small would cost more than its
     // tokens.  One thread's sequences hold either border.
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const long long border = blockIdx.x < ctas ? total * (blockIdx.x + i) / ctas : total;
+        const int c = (int)blockIdx.x + i;                       // total * c / ctas
+        const long long border = blockIdx.x < ctas ? each * c + (int)(total - each * ctas) * c / (int)ctas : total;
         if (border == total) {
             if (tid == 0) s_seq[i] = a.c.S, s_at[i] = 0, s_u[i] = total;
         } else if (border >= before && border < before + mine) {
@@ -865,7 +873,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
                 at += n;
             }
             long long off = border - at;
-            const int in = (int)(off % units);
+            const int in = (int)(off - quotient(off, units) * units);
             if (in <= kAttPairUnits + kAttSnap) off -= in;
             else if (in >= units - kAttSnap) off += units - in;
             s_u[i] = at + off;
@@ -877,7 +885,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     AttWalk walk;
     walk.u = s_u[0], walk.u1 = s_u[1], walk.seq = s_seq[0], walk.off = s_at[0];
     if (walk.u >= walk.u1) {
-        if (tid == 0) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
+        if (tid == 0 && !HALF) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
         return;
     }
 
@@ -984,8 +992,10 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             }
         }
         const bool whole = g.count == g.units;
-        if (!whole && g.tile0 == 0)                              // the last CTA whose run begins within this result
-            meta = make_int4((int)(((at + g.units - kAttSnap) * ctas - 1) / total), g.seq, g.head, g.group);
+        // the last CTA whose run begins within this result, and the one that has its first unit (borders near a result's ends lie on them)
+        const long long start = at - g.tile0;
+        const int last_cta = whole ? 0 : (int)quotient((start + g.units - kAttSnap) * ctas - 1, total);
+        if (!HALF && !whole && g.tile0 == 0) meta = make_int4(last_cta, g.seq, g.head, g.group);
         if (team != 0) continue;
         const bool broken = ld_shared(smem_u32(&s_dead)) != 0;
         float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * (D + 2);
@@ -1023,8 +1033,46 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
                 else *reinterpret_cast<float2*>(part + lr * D + d0) = make_float2(x[0], x[1]);
             }
         }
+        if (HALF && !whole) {                                    // the part that arrives last joins them all, behind this CTA's run
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) {
+                const int first_cta = (int)quotient((start + kAttPairUnits + kAttSnap + 1) * ctas - 1, total), parts = last_cta - first_cta + 1;
+                uint32_t* ticket = a.ctrl->kv_tickets + first_cta / 4;
+                const int shift = first_cta % 4 * 8;
+                if ((int)(atomicAdd(ticket, 1u << shift) >> shift & 255u) == parts - 1) {
+                    atomicSub(ticket, (uint32_t)parts << shift);
+                    s_join[g.tile0 == 0] = make_int4(first_cta, parts, g.seq, g.head);
+                }
+            }
+        }
     }
-    if (tid == 0) a.meta[blockIdx.x] = meta;
+    if (!HALF) {
+        if (tid == 0) a.meta[blockIdx.x] = meta;
+        return;
+    }
+    consumers_barrier();
+    __threadfence();
+    constexpr int kVecs = D / 4, kSeats = 32 * kAttWarps / kVecs;
+    float* sums = reinterpret_cast<float*>(meet + 32 * kAttWarps);
+    for (int k = 0; k < 2; ++k) {
+        const int4 to = s_join[k];
+        if (to.x < 0) continue;
+        const int at_once = min(rows, kSeats), share = kSeats / at_once, seat = tid / kVecs, col = tid - seat * kVecs, which = seat / share;
+        for (int r0 = 0; r0 < rows; r0 += at_once) {
+            const int row = r0 + which, turn = seat - which * share;
+            const bool live = which < at_once && row < rows;
+            JoinSum sum{make_float4(0, 0, 0, 0), -INFINITY, 0.0f};
+            if (live) sum = join_sum(a, to.x, to.y, row, col, turn, share);
+            meet[tid] = sum.o, sums[tid] = sum.m, sums[32 * kAttWarps + tid] = sum.l;
+            consumers_barrier();
+            if (live && turn == 0) {
+                for (int i = 1; i < share; ++i) join_add(sum, sums[tid + i * kVecs], sums[32 * kAttWarps + tid + i * kVecs], meet[tid + i * kVecs]);
+                join_store(a, to.z, to.w, row, col, sum);
+            }
+            consumers_barrier();                                 // (the sums have been read)
+        }
+    }
 }
 
 // The cache's keys or values as a map of (dim, token, head, page), boxes of `box` bytes of 16 or 32 tokens.
@@ -1083,7 +1131,7 @@ template <int D, bool F8>
 cudaError_t attend_rows(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
     const int wr = kv_attend_warp_rows(a.Q * a.group, D);
     if constexpr (D <= 128) {
-        if (a.Q * a.group <= 8) return attend_go<D, F8, 1, true>(a, ctas, s);
+        if (kv_attend_joins(a.Q * a.group, D)) return attend_go<D, F8, 1, true>(a, ctas, s);
         if (wr == 1) return attend_go<D, F8, 1>(a, ctas, s);
         if (wr == 4) return attend_go<D, F8, 4>(a, ctas, s);
     }

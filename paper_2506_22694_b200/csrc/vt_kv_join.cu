@@ -4,25 +4,12 @@
 // Latency-bound: a result of 37 parts is 20 KB a row, but a chain of loads for one thread.  The rows of all joined results are dealt out as
 // tasks to a fixed grid (each CTA finds them in the list that the attention kernel left, one load and one scan), and a CTA's threads
 // share a task's parts.
-#include "vt_kv.cuh"
+#include "vt_kv_join.cuh"
 
 namespace vt {
 namespace {
 
 constexpr int kThreads = 256;
-
-__device__ __forceinline__ float exp2_of(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float4 ld_cg_f4(const float* p) {
-    float4 v;
-    asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
-    return v;
-}
-// weight of a part with maximum x under the common maximum m; a part of no token (maximum -inf) has l = 0 and o = 0
-__device__ __forceinline__ float weight(float x, float m) { return x == -INFINITY ? 1.0f : exp2_of(x - m); }
 
 // A thread has four dims of a row and every `share`-th part.
 __global__ void __launch_bounds__(kThreads)
@@ -30,7 +17,7 @@ k_kv_join(const __grid_constant__ KvAttendArgs a, int warp_rows, int ctas) {
     __shared__ int s_first[kKvMaxCtas];                          // CTA with the first part of each joined result, in order
     __shared__ int s_count[kThreads / 32];
     __shared__ float4 s_o[kThreads];
-    __shared__ float s_l[kThreads + 64];                         // (the last seat may be a part of one)
+    __shared__ float s_m[kThreads], s_l[kThreads];
     griddep_launch_dependents();
     griddep_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -64,51 +51,19 @@ k_kv_join(const __grid_constant__ KvAttendArgs a, int warp_rows, int ctas) {
     const int group_rows = min(a.Q * a.group, 16 * warp_rows), d = a.c.d, vecs = d / 4, seats = kThreads / vecs;
     const int tasks = results * group_rows, each = (tasks + (int)gridDim.x - 1) / (int)gridDim.x;
     const int at_once = min(each, seats), share = at_once ? seats / at_once : 1;
-    const int64_t size = (int64_t)a.part_rows * (d + 2);
     const int seat = tid / vecs, col = tid - seat * vecs, which = seat / share, turn = seat - which * share;
     for (int t0 = blockIdx.x * each; t0 < min(tasks, ((int)blockIdx.x + 1) * each); t0 += at_once) {
         const int t = t0 + which, c = t < tasks ? s_first[t / group_rows] : 0, lr = t % group_rows;
         const int last = ld_cg_s32(&a.meta[c].x), seq = ld_cg_s32(&a.meta[c].y), head = ld_cg_s32(&a.meta[c].z), group = ld_cg_s32(&a.meta[c].w);
         const int row = group * 16 * warp_rows + lr, parts = last - c + 1;
         const bool live = which < at_once && t < min(tasks, ((int)blockIdx.x + 1) * each) && row < a.Q * a.group;
-        // part i: the second partial result of CTA c, then the first of those behind it
-        auto part = [&](int i) { return a.part + (2 * (int64_t)(c + i) + (i == 0)) * size; };
-        float4 o = make_float4(0, 0, 0, 0);
-        float l = 0.0f, top = -INFINITY;
-        if (live) {
-            const float* m = a.part + (int64_t)a.part_rows * d + lr;
-            for (int i = col; i < parts; i += vecs) top = fmaxf(top, ld_cg_f32(m + (2 * (int64_t)(c + i) + (i == 0)) * size));
-        }
-        s_l[tid] = top;                                          // (the row's maximum: its seats' threads have looked at all parts)
-        __syncthreads();
-        for (int i = 0; i < vecs; ++i) top = fmaxf(top, s_l[seat * vecs + i]);
-        if (live) {
-#pragma unroll 8
-            for (int i = turn; i < parts; i += share) {
-                const float* p = part(i);
-                const float w = weight(ld_cg_f32(p + (int64_t)a.part_rows * d + lr), top);
-                const float4 x = ld_cg_f4(p + (int64_t)lr * d + 4 * col);
-                l += w * ld_cg_f32(p + (int64_t)a.part_rows * (d + 1) + lr);
-                o.x += w * x.x, o.y += w * x.y, o.z += w * x.z, o.w += w * x.w;
-            }
-        }
-        __syncthreads();
-        s_o[tid] = o, s_l[tid] = l;
+        JoinSum s{make_float4(0, 0, 0, 0), -INFINITY, 0.0f};
+        if (live) s = join_sum(a, c, parts, lr, col, turn, share);
+        s_o[tid] = s.o, s_m[tid] = s.m, s_l[tid] = s.l;
         __syncthreads();
         if (live && turn == 0) {
-            for (int i = 1; i < share; ++i) {
-                const float4 x = s_o[tid + i * vecs];
-                o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
-                l += s_l[tid + i * vecs];
-            }
-            const int qi = row / a.group;
-            const int64_t to = ((int64_t)seq * a.Q + qi) * a.Hq + head * a.group + (row - qi * a.group);
-            const bool none = l == 0.0f;
-            const float inv = none ? 0.0f : 1.0f / l;
-            const __nv_bfloat162 x = none ? __floats2bfloat162_rn(0, 0) : __floats2bfloat162_rn(o.x * inv, o.y * inv);
-            const __nv_bfloat162 y = none ? __floats2bfloat162_rn(0, 0) : __floats2bfloat162_rn(o.z * inv, o.w * inv);
-            *reinterpret_cast<uint2*>(a.out + to * d + 4 * col) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-            if (col == 0 && a.lse) a.lse[to] = none ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+            for (int i = 1; i < share; ++i) join_add(s, s_m[tid + i * vecs], s_l[tid + i * vecs], s_o[tid + i * vecs]);
+            join_store(a, seq, head, row, col, s);
         }
         __syncthreads();                                         // (the sums have been read)
     }
@@ -140,6 +95,7 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, cudaStream_t s) {
     int ctas = 0;
     const cudaError_t e = a.c.k_exp ? launch_kv_attend_e4m3(a, ctas, s) : launch_kv_attend_bf16(a, ctas, s);
     if (e != cudaSuccess) return e;
+    if (kv_attend_joins(a.Q * a.group, a.c.d)) return cudaSuccess;
     const int wr = kv_attend_warp_rows(a.Q * a.group, a.c.d);
     const unsigned grid = (unsigned)(2 * num_sms());
     return launch_dependent(k_kv_join, grid, kThreads, 0, s, a, wr, ctas);
