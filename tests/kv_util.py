@@ -98,20 +98,20 @@ class Host:
 
     def values(self, s, index):
         """(k, v) [n, heads, d] in 64 bits of places `index` of sequence s."""
-        at = [self.place(s, i) for i in index]
+        at = torch.as_tensor(index, dtype=torch.int64)
+        p, j = self.pages[s].long()[at // self.page], at % self.page
         out = []
         for x, e in ((self.k, self.ke), (self.v, self.ve)):
-            rows = torch.stack([x.view(torch.uint8)[p, :, j] if e is not None else x[p, :, j] for p, j in at]) if at else x.new_zeros((0, self.heads, self.d))
             if e is None:
-                out.append(rows.double())
+                out.append(x[p, :, j].double())
             else:
-                ex = torch.stack([e[p, :, j] for p, j in at]) if at else e.new_zeros((0, self.heads))
-                out.append(decode(rows, ex))
+                out.append(decode(x.view(torch.uint8)[p, :, j], e[p, :, j]))
         return out
 
     def powers(self, s, index):
         """The values' powers of two [n, heads] (e4m3)."""
-        e = torch.stack([self.ve[p, :, j] for p, j in (self.place(s, i) for i in index)])
+        at = torch.as_tensor(index, dtype=torch.int64)
+        e = self.ve[self.pages[s].long()[at // self.page], :, at % self.page]
         return torch.pow(torch.tensor(2.0, dtype=torch.float64), (e.long() - 127).double())
 
     def same(self, dev=None):

@@ -26,6 +26,11 @@ def check(host, q, lens, Q, node=None, parent=None, scale=None, ws=None, flags=0
     return out, lse
 
 
+def check_again(host, q, lens, Q, node, parent):
+    dev = lambda x: None if x is None else x.cuda()
+    return vt.vt_kv_attend(q.cuda(), host.dev, host.pages_dev, torch.tensor(lens, dtype=I32).cuda(), dev(node), dev(parent))
+
+
 # one row a sequence: every head size and format, groups of query heads, page sizes that do and do not divide a tile, lengths around its edges
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("d,Hq,Hk,page", [(64, 8, 8, 16), (64, 32, 8, 7), (96, 4, 4, 32), (128, 8, 8, 16), (128, 32, 8, 64), (128, 28, 4, 5),
@@ -74,6 +79,26 @@ def test_many_sequences_of_very_different_lengths():
     lens = [(37 * i * i) % 401 if i % 7 else 0 for i in range(150)]       # (more sequences than a CTA has threads)
     host = ku.Host(150, 401, 2, 64, 16, False, seed=4)
     check(host, ku.bf16((150, 4, 64), 1), lens, 1)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d,Hq,Hk,Q,page", [(128, 4, 4, 1, 32), (128, 4, 4, 1, 16), (128, 8, 4, 8, 48), (64, 4, 4, 1, 96), (64, 16, 4, 8, 32), (256, 4, 4, 1, 64), (96, 4, 4, 1, 24)])
+def test_enough_tokens_for_many_turns_of_every_place_on_chip(d, Hq, Hk, Q, page, e4m3):
+    """About one whole result for each SM, every one of many rounds, and a tree behind each."""
+    lens = [1500 + 23 * (i % 9) for i in range(37)]
+    host = ku.Host(37, 1800, Hk, d, page, e4m3, seed=d + page)
+    node = torch.randint(-1, 20, (37 * Q,), generator=ku.gen(5)).to(I32) if Q > 1 else None
+    q = ku.bf16((37 * Q, Hq, d), 7, 1.5)
+    a = check(host, q, lens, Q, node, ku.tree(37, 20, 3) if Q > 1 else None)
+    for _ in range(3):
+        b = check_again(host, q, lens, Q, node, ku.tree(37, 20, 3) if Q > 1 else None)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_more_sequences_than_lengths_are_kept_for():
+    lens = [(7 * i) % 90 for i in range(1300)]
+    host = ku.Host(1300, 90, 1, 64, 16, True, seed=4)
+    check(host, ku.bf16((1300, 2, 64), 1), lens, 1)
 
 
 def test_a_scale_of_its_own_strided_queries_and_other_layouts():
