@@ -806,8 +806,8 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     __shared__ uint64_t s_full[C::kSlots], s_empty[C::kSlots];
     __shared__ float s_qscale[C::kQRegs ? 1 : 16 * WR];          // powers that the queries' rows were scaled by, undone in the scores
     __shared__ long long s_sum[kAttWarps + kAttFeeds];
-    __shared__ long long s_at[2], s_u[2];
-    __shared__ int s_seq[2], s_dead;
+    __shared__ long long s_at, s_u[2];
+    __shared__ int s_seq, s_dead;
     __shared__ AttWalk s_walk[kAttWarps];
     __shared__ AttSegment s_segment[kAttWarps];
     __shared__ long long s_first[kAttWarps];
@@ -825,30 +825,38 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     if (tid == 0) s_dead = 0, s_join[0].x = s_join[1].x = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     griddep_launch_dependents();
+    __syncthreads();
     griddep_wait();
     const int rows = a.Q * a.group, groups = (rows + 16 * WR - 1) / (16 * WR);
     const int64_t per_unit = (int64_t)a.c.heads * groups;
 
-    // this CTA's run of units: [u0, u1) of all sequences' units laid end to end
-    const int chunk = (a.c.S + kAttThreads - 1) / kAttThreads, sa = min(tid * chunk, a.c.S), sb = min(sa + chunk, a.c.S);
+    // This CTA's run of units: [u0, u1) of all sequences' units laid end to end.  A few sequences are looked at by every warp for itself, a lane
+    // each: two meetings of the CTA less in front of the first copy.
+    const bool few = a.c.S <= 32;
+    const int chunk = few ? 1 : (a.c.S + kAttThreads - 1) / kAttThreads, sa = min((few ? lane : tid) * chunk, a.c.S), sb = min(sa + chunk, a.c.S);
     long long mine = 0;
     for (int s = sa; s < sb; ++s) {
         const int n = att_len(a, s);
         if (s < kAttLens) lens[s] = n;
         mine += att_units(a, n);
     }
+    __syncwarp();                                                // (the lengths that other lanes have stored)
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long y = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += y;
     }
-    if (lane == 31) s_sum[warp] = incl;
-    __syncthreads();
     long long before = incl - mine, total = 0;
-    for (int w = 0; w < kAttWarps + kAttFeeds; ++w) {
-        if (w < warp) before += s_sum[w];
-        total += s_sum[w];
+    if (few) {
+        total = __shfl_sync(0xffffffffu, incl, 31);
+    } else {
+        if (lane == 31) s_sum[warp] = incl;
+        __syncthreads();
+        for (int w = 0; w < kAttWarps + kAttFeeds; ++w) {
+            if (w < warp) before += s_sum[w];
+            total += s_sum[w];
+        }
     }
     total *= per_unit;
     before *= per_unit;
@@ -857,33 +865,44 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     const long long each = quotient(total, ctas);
     // The run begins and ends where equal shares do, but not within a result's first or last units: a piece that small would cost more than its
     // tokens.  One thread's sequences hold either border.
+    AttWalk walk;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int c = (int)blockIdx.x + i;                       // total * c / ctas
         const long long border = blockIdx.x < ctas ? each * c + (int)(total - each * ctas) * c / (int)ctas : total;
-        if (border == total) {
-            if (tid == 0) s_seq[i] = a.c.S, s_at[i] = 0, s_u[i] = total;
-        } else if (border >= before && border < before + mine) {
+        const bool here = border == total ? (few ? lane : tid) == 0 : border >= before && border < before + mine;
+        long long u = total, off = 0;
+        int s = a.c.S;
+        if (here && border < total) {
             long long at = before, n = 0;
-            int s = sa, units = 0;
-            for (;; ++s) {
+            int units = 0;
+            for (s = sa;; ++s) {
                 units = att_units(a, s < kAttLens ? lens[s] : att_len(a, s));
                 n = units * per_unit;
                 if (s == sb - 1 || at + n > border) break;
                 at += n;
             }
-            long long off = border - at;
+            off = border - at;
             const int in = (int)(off - quotient(off, units) * units);
             if (in <= kAttPairUnits + kAttSnap) off -= in;
             else if (in >= units - kAttSnap) off += units - in;
-            s_u[i] = at + off;
+            u = at + off;
             if (off == n) ++s, off = 0;
-            s_seq[i] = s, s_at[i] = off;
+        }
+        if (few) {
+            const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+            u = __shfl_sync(0xffffffffu, u, from);
+            if (i == 0) walk.u = u, walk.off = __shfl_sync(0xffffffffu, off, from), walk.seq = __shfl_sync(0xffffffffu, s, from);
+            else walk.u1 = u;
+        } else if (here) {
+            s_u[i] = u;
+            if (i == 0) s_at = off, s_seq = s;
         }
     }
-    __syncthreads();
-    AttWalk walk;
-    walk.u = s_u[0], walk.u1 = s_u[1], walk.seq = s_seq[0], walk.off = s_at[0];
+    if (!few) {
+        __syncthreads();
+        walk.u = s_u[0], walk.u1 = s_u[1], walk.seq = s_seq, walk.off = s_at;
+    }
     if (walk.u >= walk.u1) {
         if (tid == 0 && !HALF) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
         return;
@@ -958,12 +977,16 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         const int row0 = g.group * 16 * WR, r0 = row0 + wr * 16 + (lane >> 2), r1 = r0 + 8;
 
         // the teams' parts meet, the upper half's with the lower half's: a lane hands its share to the lane with the same rows and dims
-        consumers_barrier();                                     // (the meeting place is free)
+        // (of a short segment's teams only the first have had tokens)
+        const int active = g.tree ? C::kTeams : min((g.token_end - g.token + C::kTile - 1) / C::kTile, C::kTeams);
+        if (active > 1 || !C::kQRegs) consumers_barrier();       // (the meeting place is free, and so are the queries' rows)
         constexpr int kShare = D / 8 + 1;                        // vectors of a lane
+        bool first_step = true;
 #pragma unroll
         for (int half = C::kTeams / 2; half >= 1; half /= 2) {
+            if (half >= active) continue;
             // who gives uses the place that it has read from: its own place, or in the first step that of the reader
-            float4* place = meet + (team >= half && half == C::kTeams / 2 ? warp - half * WR : warp) * kShare * 32 + lane;
+            float4* place = meet + (team >= half && first_step ? warp - half * WR : warp) * kShare * 32 + lane;
             if (team >= half && team < 2 * half) {
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) place[32 * i] = make_float4(acc.o[i][0], acc.o[i][1], acc.o[i][2], acc.o[i][3]);
@@ -971,7 +994,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             }
             consumers_barrier();
             if (team < half) {
-                const float4* from = half == C::kTeams / 2 ? place : place + half * WR * kShare * 32;
+                const float4* from = first_step ? place : place + half * WR * kShare * 32;
                 const float4 y = from[32 * (D / 8)];
                 const float ym[2] = {y.x, y.y}, yl[2] = {y.z, y.w};
                 float fa[2], fb[2];
@@ -990,6 +1013,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
                     acc.o[i][2] = acc.o[i][2] * fa[1] + x.z * fb[1], acc.o[i][3] = acc.o[i][3] * fa[1] + x.w * fb[1];
                 }
             }
+            first_step = false;
         }
         const bool whole = g.count == g.units;
         // the last CTA whose run begins within this result, and the one that has its first unit (borders near a result's ends lie on them)
@@ -1052,12 +1076,12 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         return;
     }
     consumers_barrier();
-    __threadfence();
     constexpr int kVecs = D / 4, kSeats = 32 * kAttWarps / kVecs;
     float* sums = reinterpret_cast<float*>(meet + 32 * kAttWarps);
     for (int k = 0; k < 2; ++k) {
         const int4 to = s_join[k];
         if (to.x < 0) continue;
+        __threadfence();                                         // (the other CTAs' parts)
         const int at_once = min(rows, kSeats), share = kSeats / at_once, seat = tid / kVecs, col = tid - seat * kVecs, which = seat / share;
         for (int r0 = 0; r0 < rows; r0 += at_once) {
             const int row = r0 + which, turn = seat - which * share;
