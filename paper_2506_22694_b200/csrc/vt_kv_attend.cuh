@@ -161,11 +161,6 @@ __device__ __forceinline__ uint32_t q_pair(uint32_t w, float f) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-template <int WR>
-__device__ __forceinline__ void team_barrier(int team) {
-    if (WR == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(32 * WR) : "memory");
-}
 __device__ __forceinline__ void consumers_barrier() { asm volatile("bar.sync 15, %0;" ::"n"(32 * kAttWarps) : "memory"); }
 
 __device__ __forceinline__ void feeds_barrier() { asm volatile("bar.sync 14, %0;" ::"n"(32 * kAttFeeds) : "memory"); }
@@ -221,7 +216,7 @@ struct AttAcc {
 // One tile: scores of the warp's 16 rows with its tokens, running maximum, weighted values.  LIST: tokens are a tree's nodes, and the
 // tile's masks say which new rows see each.  HALF: there are eight rows at the most, the lanes' second rows are none.
 template <int D, bool F8, int WR, bool HALF, bool LIST>
-__device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, uint8_t* slot, const uint8_t* note, const float (&scale)[2],
+__device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, const uint8_t* slot, const uint8_t* note, const float (&scale)[2],
                                          int qi0, int qi1) {
     using C = AttCfg<D, F8, WR>;
     constexpr int NT = C::kTile / 8;                             // groups of 8 tokens
@@ -275,17 +270,17 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int t = 8 * i + 2 * j + u;
-            float bias;
             if (F8) {
+                // (the powers of the key and of the query first: a large one may undo a small one)
                 const float4 x = *reinterpret_cast<const float4*>(note + 16 * t);
-                s[i][u] *= x.x;
-                if (!HALF) s[i][2 + u] *= x.x;
-                bias = x.y, ve[u] = x.z, vf[i][u] = x.w;
+                s[i][u] = fmaf(s[i][u], x.x * scale[0], x.y);
+                if (!HALF) s[i][2 + u] = fmaf(s[i][2 + u], x.x * scale[1], x.y);
+                ve[u] = x.z, vf[i][u] = x.w;
             } else {
-                bias = *reinterpret_cast<const float*>(note + 4 * t);
+                const float bias = *reinterpret_cast<const float*>(note + 4 * t);
+                s[i][u] = fmaf(s[i][u], scale[0], bias);
+                if (!HALF) s[i][2 + u] = fmaf(s[i][2 + u], scale[1], bias);
             }
-            s[i][u] = fmaf(s[i][u], scale[0], bias);
-            if (!HALF) s[i][2 + u] = fmaf(s[i][2 + u], scale[1], bias);
             if (LIST) {
                 const unsigned long long bits = *reinterpret_cast<const unsigned long long*>(note + C::kMasks + 8 * t);
                 const bool r0 = (bits >> qi0) & 1, r1 = (bits >> qi1) & 1;
@@ -336,19 +331,19 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
             }
         }
     }
-    uint8_t* vals = slot + C::kHalf;
+    bool odd = false;
     if (LIST && !F8) {
         // A drafted token that some of the rows see stays out of the others' sums by a weight of zero, and zero times an infinity or a NaN is
         // a NaN.  Such values are added to the rows that see them one by one, and are zeros for the MMA.
-        const int team = (int)(threadIdx.x >> 5) / WR;
-        bool odd = false;
+        const uint8_t* vals = slot + C::kHalf;
         for (int x = lane; x < C::kTile * (D / 8); x += 32) {
             const uint4 w = *reinterpret_cast<const uint4*>(vals + C::place(x / (D / 8), x % (D / 8)));
             const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) odd |= (ws[i] & 0x7f80u) == 0x7f80u || (ws[i] & 0x7f800000u) == 0x7f800000u;
         }
-        if (__any_sync(0xffffffffu, odd)) {                      // (every warp of the team sees the same tile)
+        odd = __any_sync(0xffffffffu, odd);
+        if (odd) {
 #pragma unroll
             for (int i = 0; i < NT; ++i)
                 for (int t = 0; t < 8; t += 2) {                 // tokens t and t + 1 of the eight, from the lane that holds them
@@ -370,13 +365,6 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                             }
                     }
                 }
-            team_barrier<WR>(team);
-            for (int x = lane; x < C::kTile * D; x += 32) {      // (every warp of the team writes the same zeros)
-                uint16_t* at = reinterpret_cast<uint16_t*>(vals + C::place(x / D, x % D / 8)) + x % 8;
-                if ((*at & 0x7f80u) == 0x7f80u) *at = 0;
-            }
-            fence_async();
-            team_barrier<WR>(team);
         }
     }
     // bf16: weights go into the MMA as two pieces, the rounded weight and what the rounding left (2^-17 of it at most): one piece alone would
@@ -402,6 +390,10 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
         for (int c = 0; c < C::kRow / 32; ++c) {
             uint32_t b[4];
             ldsm_t(b, v_at + (v_vec ^ (2 * c % kVecs << 4)) + 2 * c / kVecs * (C::kTile * C::kBox) + g * 16 * C::kBox);
+            if (LIST && !F8 && odd) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] &= ((b[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((b[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+            }
             if (!F8) {
                 mma<false>(acc.o[2 * c], hi, b[0], b[1]);
                 mma<false>(acc.o[2 * c + 1], hi, b[2], b[3]);
@@ -462,7 +454,7 @@ __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens,
 
 // A producer's lane: its tokens of a round, one of each tile.
 struct AttTokens {
-    int32_t id[kAttTurns], in[kAttTurns];                        // page (-1: out of range, -2: no token) and place in it
+    int32_t id[kAttTurns], in[kAttTurns];                        // page (below 0: no row to read) and place in it (-1: no token)
     unsigned long long mask[kAttTurns];                          // a tree's token: the rows that see it
     uint32_t ke[kAttTurns], ve[kAttTurns];                       // e4m3: its exponents' bytes
     int head, n;                                                 // tokens of the round
@@ -525,7 +517,7 @@ struct AttProducer {
         }
 #pragma unroll
         for (int t = 0; t < kAttTurns; ++t) {
-            r.id[t] = -2, r.in[t] = 0;
+            r.id[t] = r.in[t] = -1;
             if (index[t] < 0) continue;
             const uint32_t page = a.page_shift >= 0 ? (uint32_t)index[t] >> a.page_shift : (uint32_t)index[t] / (uint32_t)a.c.page;
             r.in[t] = index[t] - (int32_t)(page * (uint32_t)a.c.page);
@@ -559,9 +551,9 @@ struct AttProducer {
     __device__ void resolve(AttTokens& r) {
 #pragma unroll
         for (int t = 0; t < kAttTurns; ++t) {
-            if (r.id[t] != -2 && (uint32_t)r.id[t] >= (uint32_t)a.c.n_pages) {
-                kv_flag(a.ctrl);
-                r.id[t] = -2;
+            if ((uint32_t)r.id[t] >= (uint32_t)a.c.n_pages) {
+                if (r.in[t] >= 0) kv_flag(a.ctrl);
+                r.id[t] = -1;
             }
             if (F8) {
                 // (fewer than 2^31 rows fit any GPU's memory)
@@ -941,7 +933,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         for (bool more = true; more;) {
             const int slot = feed * C::kPer + place;
             att_wait(smem_u32(s_full) + 8 * slot, parity, smem_u32(&s_dead), a.ctrl);
-            uint8_t* tile = ring + slot * C::kSlot;
+            const uint8_t* tile = ring + slot * C::kSlot;
             const uint8_t* note = notes + slot * C::kNote;
             const uint32_t header = ld_shared(smem_u32(note) + C::kHeader);
             if (!(header & kAttEmpty)) {

@@ -309,3 +309,64 @@ def test_no_sequences():
     dev = host.device()
     out, lse = vt.vt_kv_attend(torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda"), dev, host.pages_dev[:0], torch.empty(0, dtype=I32, device="cuda"))
     assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+
+
+@pytest.mark.parametrize("page_id", [-1, -2, -3, -2 ** 31, 2 ** 31 - 1])
+def test_any_page_id_out_of_range_is_flagged(page_id):
+    for e4m3 in (False, True):
+        host = ku.Host(1, 40, 1, 64, 16, e4m3, seed=8)
+        broken = host.pages.clone()
+        broken[0, 1] = page_id
+        q, ws = ku.bf16((1, 2, 64), 2), ku.attend_ws(1, 1, 2, 1, 64)
+        out, _ = vt.vt_kv_attend(q.cuda(), host.device(), broken.cuda(), torch.tensor([32], dtype=I32).cuda(), ws=ws)
+        assert ws.read_status()[1] == vt.VT_FLAG_BAD_PAGE
+        ref, _, tol, _ = ku.attend(host, q, [16], 1)                      # (what the first page holds)
+        ok, worst = ku.near(out, ref, tol)
+        assert ok, worst
+
+
+@pytest.mark.parametrize("power", [106, -106])
+def test_powers_of_queries_and_keys_that_undo_each_other(power):
+    """Keys of 2^113 (their sum with a query of 2^14 in f16 would not fit fp32) under queries of 2^-112, and the other way round."""
+    for Hq in (2, 32):
+        host = ku.Host(2, 70, 2, 64, 16, True, seed=4)
+        host.ke = torch.full_like(host.ke, 127 + power)
+        q = (ku.bf16((2, Hq, 64), 3).float() * 2.0 ** (-power - 6)).to(torch.bfloat16)
+        check(host, q, [70, 9], 1)
+
+
+@pytest.mark.parametrize("S", [31, 32, 33, 384, 385])
+def test_sequences_about_the_numbers_at_which_they_are_dealt_out_otherwise(S):
+    for Q in (1, 9):
+        host = ku.Host(S, 40, 1, 64, 8, False, seed=S)
+        lens = [(7 * s) % 41 for s in range(S)]
+        lens[-1] = 0
+        check(host, ku.bf16((S * Q, 2, 64), 6), lens, Q)
+
+
+def test_two_captured_calls_share_a_workspace():
+    """Their partial results lie in the same places: replays in turn, on one stream, are what the calls give by themselves."""
+    a, b = ku.Host(1, 4000, 2, 64, 16, False, seed=1), ku.Host(3, 2500, 2, 64, 16, False, seed=2)
+    ws = ku.attend_ws(3, 9, 4, 2, 64)
+    calls = []
+    for host, Q, lens in ((a, 1, [4000]), (b, 9, [2500, 0, 1700]), (b, 2, [31, 2222, 1])):
+        q = ku.bf16((host.S * Q, 4, 64), Q).cuda()
+        dev, n = host.device(), torch.tensor(lens, dtype=I32).cuda()
+        out = (torch.empty_like(q), torch.empty(q.shape[:2], device="cuda"))
+        call = lambda q=q, dev=dev, pages=host.pages_dev, n=n, out=out: vt.vt_kv_attend(q, dev, pages, n, out=out, ws=ws)
+        call()
+        torch.cuda.synchronize()
+        want = [x.clone() for x in out]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        calls.append((graph, out, want, call))                            # (whose tensors the graph reads)
+    for _ in range(3):
+        for graph, out, _w, _c in calls:
+            for x in out:
+                x.zero_()
+            graph.replay()
+    torch.cuda.synchronize()
+    for _g, out, want, _c in calls:
+        assert all(torch.equal(x, y) for x, y in zip(out, want))
+    assert ws.read_status()[1] == 0

@@ -152,6 +152,9 @@ def test_write_leaves_out_what_is_out_of_range_and_says_so():
         write(host, 3, 4, [1, -1, -2 ** 31], [0, 0, 5], [0, 0, 0], 64, ws=ws)                  # (negative places are nobody's error)
         for seq, index in ((2, 0), (-1, 0), (0, 30), (0, 2 ** 31 - 1), (1, 25)):
             write(host, 2, 4, [index, 3], [seq, 1], [1, 2], 64, ws=ws, flags=vt.VT_FLAG_BAD_PAGE)
+        for page in (-1, -2, -2 ** 31):
+            host.pages[1, 2] = page
+            write(host, 2, 4, [25, 3], [1, 1], [1, 2], 64, ws=ws, flags=vt.VT_FLAG_BAD_PAGE)
 
 
 def test_queries_in_place():
