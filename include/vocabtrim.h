@@ -345,8 +345,8 @@ vt_status vt_draft_head_host(const uint16_t *h_host, const uint16_t *W_trim, con
  *   pages         DEVICE int32 [S, max_pages], rows pages_ld >= max_pages apart; max_pages * page < 2^31.
  *
  * Sequences, places, pages and nodes out of range are left out (not written, not seen, read as zeros) and
- * raise VT_FLAG_BAD_PAGE in the workspace, where one is given.  Two rows of a call for the same place, or a page
- * that two sequences write, leave either row's bytes.
+ * raise VT_FLAG_BAD_PAGE in the workspace, where one is given.  A place that two rows of one call write, directly or
+ * through a page of two sequences, holds no particular row afterwards; pages that are only read may be shared.
  */
 #define VT_KV_BF16 0
 #define VT_KV_E4M3 1
@@ -412,7 +412,8 @@ vt_status vt_kv_read(const vt_kv_cache *cache, const int32_t *seq, const int32_t
  *     NULL: chains (parent[i] = i - 1).  N <= VT_KV_MAX_NODES; N is looked at with `node` only.
  *   out [S*Q,Hq,d] bf16; lse [S*Q,Hq] fp32 or NULL.  A row whose weights sum to zero (it sees no token, or scores of -inf) has
  *     zeros and an lse of -inf.
- * Sums, maxima and scores are fp32, weights enter the products as two bf16 pieces.  Sequences may have any lengths;
+ * Sums, maxima and scores are fp32; weights enter the products as two bf16 pieces (what is lost is 2^-17 of one), over an
+ * e4m3 cache as one f16 number (2^-11).  out must not overlap q or the cache.  Sequences may have any lengths;
  * results are the same from call to call.  Workspace: vt_workspace_bytes(VT_OP_KV_ATTEND, ...).
  */
 vt_status vt_kv_attend(const uint16_t *q, int64_t q_ld, int32_t Q, int32_t Hq, const vt_kv_cache *cache, const int32_t *lens,

@@ -7,19 +7,25 @@
 // One pass with a running maximum; what is kept of a part (maximum m in base 2, sum l, weighted values o) joins with another part by
 // m' = max, l' = l 2^(m - m') + ..., o' likewise.
 //
-// Bound: HBM, 2 * d * (2 or 1) bytes of a token and key head, each read once for all rows that share the head.  So rows of a key head
+// Bound: HBM, 2 * d * (2 or 1) bytes of a token and key head, each read once for all rows that share the head.  So the rows of a key head
 // (its query heads times the sequence's new rows) lie side by side as the 16 rows of an MMA, up to four such groups (WR) on warps that share
 // the tiles.  mma.sync is far from its own limit at 16 and 32 rows (a token and head is two MMAs in the 22 cycles in which an SM's share of HBM
 // delivers it), and it keeps scores and weights in registers, where tcgen05 would send both through TMEM for tiles of 128 rows that
 // are seven eighths empty.
 //
+// Measured (heads of 128, 8 key heads): 64 sequences of up to 8000 tokens, bf16, 172 us, 92% of what copying HBM reaches; e4m3 106 us, 75%: there the
+// producers' instructions bound it (a tile has half the bytes and the exponents on top).  One sequence of 4001 tokens: 12.6 us, of which 8 are
+// what a call of 64 tokens takes: launch 2.5, lengths 1.6, queries and first page ids 0.9, first tile 1.5, meeting and end 2.
+//
 // Split: the work is cut into units of 64 tokens, in the order (sequence, key head, group of rows, tokens), and every CTA takes an equal run of
 // units, whatever the lengths are; nothing is known to the host, so a captured graph stays right when lengths change.  A (sequence, head, group)
-// whose units lie in several CTAs leaves partial results, which a second launch joins in the order of the tokens.
+// whose units lie in several CTAs leaves partial results.  Those of up to eight rows are joined by the CTA whose part comes last, others by a
+// second launch; always in the order of the tokens.
 //
-// Roles: four producer warps walk the CTA's run, look pages up, and fill rings of tiles by tensor copies of 16 tokens, as far ahead as the rings reach
-// (copies of a row each took 10 ns apiece, twice what there is); eight warps consume, as 8 / WR teams that take the tiles in turn.  So the copies go on while a result is finished and the next one's queries are
-// fetched, which took 5 us a result when the same warps did both.
+// Roles: four producer warps walk the CTA's run, look pages up, and fill rings of tiles by tensor copies of 16 or 32 tokens, as far ahead as
+// the rings reach (copies of a row each took 10 ns apiece, twice what there is).  Eight warps consume, as 8 / WR teams that take the tiles in
+// turn.  So the copies go on while a result is finished and the next one's queries are fetched, which took 5 us a result when the same warps
+// did both.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -83,8 +89,8 @@ struct AttCfg {
         return vec / kVecs * (kTile * kBox) + row * kBox + ((vec % kVecs ^ swizzle(row)) << 4);
     }
 };
-// What an e4m3 tile holds of a token (bf16: the second alone): the factor of its score, 0 or (no such token) -inf to be added, the
-// exponent of its values within what keeps all weights finite, and their power of two (0: no such token).
+// What an e4m3 tile holds of a token (bf16: the second alone): the power of two of its key (0: no such token), 0 or (no such token) -inf to be
+// added to its score, the exponent of its values within what keeps all weights finite, and their power of two (0: no such token).
 enum { kAttEnd = 1, kAttEmpty = 2, kAttTree = 4 };               // a tile's header
 
 // One lane of a converged warp: the compiler then knows that one thread is active.
@@ -452,6 +458,10 @@ __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens,
     return true;
 }
 
+enum { kChain, kLevels, kNodes };                                // how a producer finds a tree's nodes
+constexpr int kAttDeep = 64;                                     // depths that are walked in step
+constexpr int kAttHeld = 1;                                      // parents that a producer's lane asks for at a time
+
 // A producer's lane: its tokens of a round, one of each tile.
 struct AttTokens {
     int32_t id[kAttTurns], in[kAttTurns];                        // page (below 0: no row to read) and place in it (-1: no token)
@@ -473,7 +483,12 @@ struct AttProducer {
     AttSegment g;
     int groups, lane, feed;
     int mode;                     // 0: the next segment, 1: committed tokens, 2: the tree's
-    int tree_of, n0, n1, f0, f1;  // whose parents are here; nodes of rows lane and lane + 32, and where they have got to
+    int tree_of, n0, n1;          // whose tree is here; nodes of rows lane and lane + 32
+    int f0, f1;                   // where those have got to
+    int way = 0, depth = 0, most = 0;                            // how nodes are found; of row lane's node (-1: none), and of all rows'
+    int level = 0;                // where the search is
+    int held[kAttHeld];           // parents on their way
+    bool fresh = false, begun = false;                           // the tree's loads are in flight; the segment's tree has been begun
     int place = 0, filled = 0;    // of the next tile, in the ring; tiles so far
     uint32_t parity = 1;          // (an empty ring's places count as given back)
     unsigned long long dirty = 0; // places that hold rows which threads have stored
@@ -486,7 +501,8 @@ struct AttProducer {
             r.have = att_next(a, lens, groups, walk, g);
             if (!r.have) return;
             mode = g.token >= g.token_end && g.tree ? 2 : 1;
-            if (g.tree) load_tree();
+            begun = false;
+            if (g.tree && tree_of != g.seq) ask_tree();
         }
         r.have = true, r.head = g.head, r.tree = mode == 2;
         int index[kAttTurns];
@@ -501,18 +517,58 @@ struct AttProducer {
             r.last = g.token >= g.token_end && !g.tree;
             if (g.token >= g.token_end) mode = g.tree ? 2 : 0;
         } else {
-            // the nodes that some row sees, largest first: the rows' walks to the root are merged (by every producer, for its own tokens)
-            for (r.n = 0; r.n < kAttRound; ++r.n) {
-                const int f = __reduce_max_sync(0xffffffffu, max(f0, f1));
-                if (f < 0) break;
-                const unsigned lo = __ballot_sync(0xffffffffu, f0 == f), hi = __ballot_sync(0xffffffffu, f1 == f);
+            if (!begun) begin_tree();
+            begun = true;
+            r.n = 0;
+            if (way == kChain) {                                 // every node up to the largest
+                r.n = min(most - level, kAttRound);
 #pragma unroll
                 for (int t = 0; t < kAttTurns; ++t)
-                    if (r.n == mine(t)) index[t] = (int32_t)min((int64_t)g.len + f, (int64_t)INT32_MAX), r.mask[t] = ((unsigned long long)hi << 32) | lo;
-                const int up = a.parent ? (int)parents[f] : f - 1;
-                f0 = f0 == f ? up : f0, f1 = f1 == f ? up : f1;
+                    if (mine(t) < r.n) index[t] = place_of(level + mine(t));
+#pragma unroll 1
+                for (int row = 0; row < a.Q; ++row) {
+                    const int f = __shfl_sync(0xffffffffu, row < 32 ? n0 : n1, row & 31);
+#pragma unroll
+                    for (int t = 0; t < kAttTurns; ++t)
+                        if (level + mine(t) <= f) r.mask[t] |= 1ull << row;
+                }
+                level += r.n;
+                r.last = level >= most;
+            } else if (way == kLevels) {                         // a depth at a time, deepest first
+                for (; level > 0 && r.n + 32 <= kAttRound; --level) {
+                    const bool here = depth >= level;
+                    const unsigned same = __match_any_sync(0xffffffffu, here ? f0 : -1 - lane);
+                    const unsigned first = __ballot_sync(0xffffffffu, here && (same & ((1u << lane) - 1)) == 0);
+                    const int count = __popc(first);
+#pragma unroll
+                    for (int t = 0; t < kAttTurns; ++t) {
+                        const int k = mine(t) - r.n;             // which of the depth's nodes is this lane's
+                        if (!__any_sync(0xffffffffu, k >= 0 && k < count)) continue;
+                        int from = 0;
+#pragma unroll
+                        for (int w = 16; w; w >>= 1)
+                            if (__popc(first & ((1u << (from + w)) - 1)) <= k) from += w;
+                        const int f = __shfl_sync(0xffffffffu, f0, from & 31);
+                        const unsigned rows = __shfl_sync(0xffffffffu, same, from & 31);
+                        if (k >= 0 && k < count) index[t] = place_of(f), r.mask[t] = rows;
+                    }
+                    r.n += count;
+                    if (here) f0 = parents[f0];
+                }
+                r.last = level <= 0;
+            } else {                                             // one by one, largest first
+                for (; r.n < kAttRound; ++r.n) {
+                    const int f = __reduce_max_sync(0xffffffffu, max(f0, f1));
+                    if (f < 0) break;
+                    const unsigned lo = __ballot_sync(0xffffffffu, f0 == f), hi = __ballot_sync(0xffffffffu, f1 == f);
+#pragma unroll
+                    for (int t = 0; t < kAttTurns; ++t)
+                        if (r.n == mine(t)) index[t] = place_of(f), r.mask[t] = ((unsigned long long)hi << 32) | lo;
+                    const int up = parents[f];
+                    f0 = f0 == f ? up : f0, f1 = f1 == f ? up : f1;
+                }
+                r.last = __reduce_max_sync(0xffffffffu, max(f0, f1)) < 0;
             }
-            r.last = __reduce_max_sync(0xffffffffu, max(f0, f1)) < 0;
             if (r.last) mode = 0;
         }
 #pragma unroll
@@ -525,26 +581,52 @@ struct AttProducer {
         }
     }
 
-    __device__ void load_tree() {
-        if (tree_of != g.seq) {
-            tree_of = g.seq;
+    __device__ int place_of(int f) const { return (int)min((int64_t)g.len + f, (int64_t)INT32_MAX); }
+
+    // A sequence's tree: loads that are left in flight while the committed tokens are looked up, ...
+    __device__ void ask_tree() {
+        tree_of = g.seq, fresh = true;
+        n0 = lane < a.Q ? ld_cg_s32(a.node + (int64_t)g.seq * a.Q + lane) : -1;
+        n1 = lane + 32 < a.Q ? ld_cg_s32(a.node + (int64_t)g.seq * a.Q + lane + 32) : -1;
+        if (!a.parent) return;
+#pragma unroll
+        for (int k = 0; k < kAttHeld; ++k) {
+            const int i = 32 * (kAttFeeds * k + feed) + lane;
+            held[k] = i < a.N ? ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i) : -1;
+        }
+    }
+    // ... and what it takes to find the nodes that some row sees, each once, with the rows that see it: of a chain all up to the largest; in a
+    // tree the rows (32 at the most) walk to the root in step, by depth; where there are more rows or a node lies deep, they are merged node by
+    // node.  Every producer finds them all, for its own tokens.  Against node by node for all: 8 sequences of 512 tokens with a chain
+    // of 64 rows each 52 us for 55, one of 1000 tokens with 32 rows in a tree of 200 nodes 22.2 for 23.7.
+    __device__ void begin_tree() {
+        if (fresh) {
+            fresh = false;
             const int N = a.N;
+            if (n0 >= N || n1 >= N) kv_flag(a.ctrl);
+            n0 = n0 < 0 || n0 >= N ? -1 : n0, n1 = n1 < 0 || n1 >= N ? -1 : n1;
+            way = kChain;
+            most = __reduce_max_sync(0xffffffffu, max(n0, n1)) + 1;
             if (a.parent) {
                 feeds_barrier();                                 // (the others have done with the parents before)
-                for (int i = 32 * feed + lane; i < N; i += 32 * kAttFeeds) {               // (a parent that does not lie in front ends the walk)
-                    const int p = ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i);
-                    parents[i] = (int16_t)(p >= 0 && p < i ? p : -1);
+                auto keep = [&](int i, int p) {
+                    if (i < N) parents[i] = (int16_t)(p >= 0 && p < i ? p : -1);           // (a parent that does not lie in front ends the walk)
+                };
+#pragma unroll
+                for (int k = 0; k < kAttHeld; ++k) keep(32 * (kAttFeeds * k + feed) + lane, held[k]);
+                for (int i = 32 * (kAttFeeds * kAttHeld + feed) + lane; i < N; i += 32 * kAttFeeds)
+                    keep(i, ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i));
+                feeds_barrier();
+                way = a.Q > 32 ? kNodes : kLevels;
+                depth = most = 0;
+                for (int f = n0; way == kLevels && __any_sync(0xffffffffu, f >= 0); ++most) {
+                    if (most == kAttDeep) way = kNodes;
+                    if (f >= 0) f = parents[f], ++depth;
                 }
             }
-            auto node = [&](int row) {
-                const int f = row < a.Q ? ld_cg_s32(a.node + (int64_t)g.seq * a.Q + row) : -1;
-                if (f >= N) kv_flag(a.ctrl);
-                return f < 0 || f >= N ? -1 : f;
-            };
-            n0 = node(lane), n1 = node(lane + 32);
-            if (a.parent) feeds_barrier();
         }
         f0 = n0, f1 = n1;
+        level = way == kLevels ? most : 0;
     }
 
     // page ids -> exponents (left in flight, too)
@@ -635,7 +717,7 @@ struct AttProducer {
             const uint32_t bias = ok ? 0u : 0xff800000u;
             if (F8) {
                 const float ve = (float)min(max((int)r.ve[turn] - 127, -100), 112);
-                st_shared(at + 16 * lane, make_uint4(__float_as_uint(kv_two_to(r.ke[turn])), bias, __float_as_uint(ve), ok ? __float_as_uint(kv_two_to(r.ve[turn])) : 0u));
+                st_shared(at + 16 * lane, make_uint4(ok ? __float_as_uint(kv_two_to(r.ke[turn])) : 0u, bias, __float_as_uint(ve), ok ? __float_as_uint(kv_two_to(r.ve[turn])) : 0u));
             } else {
                 st_shared(at + 4 * lane, bias);
             }
@@ -970,7 +1052,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
 
         // the teams' parts meet, the upper half's with the lower half's: a lane hands its share to the lane with the same rows and dims
         // (of a short segment's teams only the first have had tokens)
-        const int active = g.tree ? C::kTeams : min((g.token_end - g.token + C::kTile - 1) / C::kTile, C::kTeams);
+        const int active = min((max(g.token_end - g.token, g.tree ? a.N : 0) + C::kTile - 1) / C::kTile, C::kTeams);
         if (active > 1 || !C::kQRegs) consumers_barrier();       // (the meeting place is free, and so are the queries' rows)
         constexpr int kShare = D / 8 + 1;                        // vectors of a lane
         bool first_step = true;

@@ -370,3 +370,44 @@ def test_two_captured_calls_share_a_workspace():
     for _g, out, want, _c in calls:
         assert all(torch.equal(x, y) for x, y in zip(out, want))
     assert ws.read_status()[1] == 0
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("Q,strands,depth", [(32, 32, 31), (8, 8, 64), (8, 8, 65), (33, 33, 20), (64, 40, 9), (20, 4, 50)])
+def test_strands_of_nodes_that_take_many_rounds(Q, strands, depth, e4m3):
+    """Node i hangs on node i - strands: many nodes at each depth, more of them than are looked up at a time, rows that end at any depth."""
+    N = strands * depth
+    host = ku.Host(2, N + 40, 1, 64, 16, e4m3, seed=Q)
+    parent = torch.arange(-strands, N - strands, dtype=I32).clamp(min=-1).repeat(2, 1)
+    node = torch.randint(0, N, (2 * Q,), generator=ku.gen(depth)).to(I32)
+    node[:Q] = N - 1 - torch.arange(Q, dtype=I32)
+    node[Q] = -1
+    check(host, ku.bf16((2 * Q, 2, 64), 5), [33, 0], Q, node, parent)
+
+
+@pytest.mark.parametrize("d,Hq,Hk,Q", [(64, 4, 4, 64), (128, 8, 2, 64), (128, 4, 4, 5), (256, 2, 1, 33)])
+def test_a_block_of_tokens_sees_what_lies_in_front(d, Hq, Hk, Q):
+    """Row i is node i of a chain: causal attention inside the block."""
+    host = ku.Host(3, 300 + Q, Hk, d, 16, False, seed=Q)
+    check(host, ku.bf16((3 * Q, Hq, d), 5), [0, 17, 300], Q, torch.arange(Q, dtype=I32).repeat(3))
+
+
+def test_an_eight_bit_row_that_no_sequence_has_does_not_matter():
+    """Not even the cache's first row, marked as no number, where tiles are filled up behind the last token or a page is missing."""
+    for Hq, Q in ((2, 1), (16, 1), (64, 1), (2, 3)):
+        host = ku.Host(2, 60, 2, 64, 16, True, seed=2)
+        free = min(set(range(1, host.k.shape[0])) - set(host.pages.flatten().tolist()))
+        for x in (host.k.view(torch.uint8), host.v.view(torch.uint8), host.ke, host.ve):   # page 0's owner, if any, takes a free page
+            x[free] = x[0]
+        host.pages[host.pages == 0] = free
+        host.ke[0], host.ve[0] = 255, 255
+        host.k.view(torch.uint8)[0], host.v.view(torch.uint8)[0] = 0x7f, 0xff
+        node = None if Q == 1 else torch.tensor([0, 4, -1] * 2, dtype=I32)
+        out, _ = check(host, ku.bf16((2 * Q, Hq, 64), 3), [5, 33], Q, node)
+        assert bool(torch.isfinite(out).all())
+        broken = host.pages.clone()
+        broken[1, 1] = -1
+        ws = ku.attend_ws(2, Q, Hq, 2, 64)
+        out, _ = vt.vt_kv_attend(ku.bf16((2 * Q, Hq, 64), 3).cuda(), host.dev, broken.cuda(), torch.tensor([5, 33], dtype=I32).cuda(),
+                                 None if node is None else node.cuda(), ws=ws)
+        assert bool(torch.isfinite(out).all()) and ws.read_status()[1] == vt.VT_FLAG_BAD_PAGE
