@@ -61,6 +61,8 @@ struct KvAttendArgs {
     const uint16_t* q;            // [S * Q, Hq, d], rows q_ld elements apart
     int64_t q_ld;
     int32_t Q, Hq, group, N;      // rows a sequence, query heads (and those of a key head), nodes a sequence
+    float inv_group;
+    bool few;                     // few enough sequences and units for 32 bits and a warp
     const int32_t *lens, *node, *parent;
     int64_t parent_ld;
     int32_t page_shift, box;      // log2 of the page where it is a power of two, else -1; tokens of a tensor copy: 32, 16 or (other pages) 0
@@ -95,6 +97,8 @@ __device__ __forceinline__ bool kv_place(const KvView& c, int64_t seq, int64_t i
     exp_at = (int64_t)id * c.heads * c.page + in;
     return true;
 }
+// Which of a sequence's new rows row `row` of a key head belongs to: row / group, of fewer than 2^21 rows (the product is off by under half a row).
+__device__ __forceinline__ int kv_row_of(const KvAttendArgs& a, int row) { return (int)(((float)row + 0.5f) * a.inv_group); }
 __device__ __forceinline__ void kv_flag(Ctrl* ctrl) {
     if (ctrl) atomicOr(&ctrl->flags, (uint32_t)VT_FLAG_BAD_PAGE);
 }

@@ -420,6 +420,7 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
 }
 
 // Quotients of numbers that nearly always fit 32 bits (a division of 64 takes some hundred instructions).
+__device__ __forceinline__ int quotient(int x, int y) { return (int)((uint32_t)x / (uint32_t)y); }
 __device__ __forceinline__ long long quotient(long long x, long long y) {
     return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
@@ -446,10 +447,10 @@ __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens,
     g.seq = w.seq;
     g.len = g.seq < kAttLens ? lens[g.seq] : att_len(a, g.seq);
     g.units = att_units(a, g.len);
-    const int pair = (int)quotient(w.off, g.units);
+    const int pair = (int)quotient(w.off, (long long)g.units);
     g.tile0 = (int)(w.off - (long long)pair * g.units);
     g.count = (int)min((long long)(g.units - g.tile0), w.u1 - w.u);
-    g.head = pair / groups, g.group = pair - g.head * groups;
+    g.head = groups == 1 ? pair : pair / groups, g.group = pair - g.head * groups;
     g.token = (int)min((long long)max(g.tile0 - kAttPairUnits, 0) * kAttUnit, (long long)g.len);
     g.token_end = (int)min((long long)max(g.tile0 + g.count - kAttPairUnits, 0) * kAttUnit, (long long)g.len);
     g.tree = a.node && g.tile0 + g.count == g.units;
@@ -783,7 +784,7 @@ struct AttQueries {
     uint2 w[C::kQRegs ? 1 : kLines][kWords];
 
     __device__ __forceinline__ static const uint16_t* row_of(const KvAttendArgs& a, const AttSegment& g, int row) {
-        const int rows = a.Q * a.group, r = min(row, rows - 1), qi = r / a.group;
+        const int rows = a.Q * a.group, r = min(row, rows - 1), qi = kv_row_of(a, r);
         return a.q + ((int64_t)g.seq * a.Q + qi) * a.q_ld + (int64_t)(g.head * a.group + (r - qi * a.group)) * D;
     }
     __device__ __forceinline__ void fetch(const KvAttendArgs& a, const AttSegment& g, int warp, int lane) {
@@ -904,76 +905,91 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     const int rows = a.Q * a.group, groups = (rows + 16 * WR - 1) / (16 * WR);
     const int64_t per_unit = (int64_t)a.c.heads * groups;
 
-    // This CTA's run of units: [u0, u1) of all sequences' units laid end to end.  A few sequences are looked at by every warp for itself, a lane
-    // each: two meetings of the CTA less in front of the first copy.
-    const bool few = a.c.S <= 32;
-    const int chunk = few ? 1 : (a.c.S + kAttThreads - 1) / kAttThreads, sa = min((few ? lane : tid) * chunk, a.c.S), sb = min(sa + chunk, a.c.S);
-    long long mine = 0;
-    for (int s = sa; s < sb; ++s) {
-        const int n = att_len(a, s);
-        if (s < kAttLens) lens[s] = n;
-        mine += att_units(a, n);
-    }
-    __syncwarp();                                                // (the lengths that other lanes have stored)
-    long long incl = mine;
+    // This CTA's run of units: [walk.u, walk.u1) of all sequences' units laid end to end.  The run begins and ends where equal shares do, but
+    // not within a result's first or last units: a piece that small would cost more than its tokens.
+    AttWalk walk;
+    long long total, ctas;
+    auto snapped = [&](auto off, int units) {                    // a border's place in its sequence
+        const int in = (int)(off - quotient(off, decltype(off)(units)) * units);
+        return in <= kAttPairUnits + kAttSnap ? off - in : in >= units - kAttSnap ? off + (units - in) : off;
+    };
+    if (a.few) {
+        // A few sequences, whose units times 148 fit 31 bits, are looked at by every warp for itself, a lane each: the first copy waits for this,
+        // and with 64-bit numbers and two meetings of the CTA it took 1.5 us.
+        const int n = lane < a.c.S ? att_len(a, lane) : 0, units = lane < a.c.S ? att_units(a, n) : 0, mine = units * (int)per_unit;
+        lens[lane] = n;                                          // (every warp stores the same)
+        __syncwarp();
+        int incl = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-    }
-    long long before = incl - mine, total = 0;
-    if (few) {
-        total = __shfl_sync(0xffffffffu, incl, 31);
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        const int all = __shfl_sync(0xffffffffu, incl, 31), parts = min((int)gridDim.x, all);
+        total = all, ctas = parts;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = min((int)blockIdx.x + i, parts), border = (int)((uint32_t)(all * c) / (uint32_t)parts);
+            int seq = __ffs(__ballot_sync(0xffffffffu, border < incl)) - 1, u = all, off = 0;
+            if (seq >= 0) {
+                const int from = __shfl_sync(0xffffffffu, incl - mine, seq);
+                off = snapped(border - from, __shfl_sync(0xffffffffu, units, seq));
+                u = from + off;
+                if (off == __shfl_sync(0xffffffffu, mine, seq)) ++seq, off = 0;
+            }
+            if (i == 0) walk.u = u, walk.off = off, walk.seq = seq;
+            else walk.u1 = u;
+        }
     } else {
+        const int chunk = (a.c.S + kAttThreads - 1) / kAttThreads, sa = min(tid * chunk, a.c.S), sb = min(sa + chunk, a.c.S);
+        long long mine = 0;
+        for (int s = sa; s < sb; ++s) {
+            const int n = att_len(a, s);
+            if (s < kAttLens) lens[s] = n;
+            mine += att_units(a, n);
+        }
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
         if (lane == 31) s_sum[warp] = incl;
         __syncthreads();
+        long long before = incl - mine;
+        total = 0;
         for (int w = 0; w < kAttWarps + kAttFeeds; ++w) {
             if (w < warp) before += s_sum[w];
             total += s_sum[w];
         }
-    }
-    total *= per_unit;
-    before *= per_unit;
-    mine *= per_unit;
-    const long long ctas = min((long long)gridDim.x, total);
-    const long long each = quotient(total, ctas);
-    // The run begins and ends where equal shares do, but not within a result's first or last units: a piece that small would cost more than its
-    // tokens.  One thread's sequences hold either border.
-    AttWalk walk;
+        total *= per_unit;
+        before *= per_unit;
+        mine *= per_unit;
+        ctas = min((long long)gridDim.x, total);
+        const long long each = quotient(total, ctas);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int c = (int)blockIdx.x + i;                       // total * c / ctas
-        const long long border = blockIdx.x < ctas ? each * c + (int)(total - each * ctas) * c / (int)ctas : total;
-        const bool here = border == total ? (few ? lane : tid) == 0 : border >= before && border < before + mine;
-        long long u = total, off = 0;
-        int s = a.c.S;
-        if (here && border < total) {
-            long long at = before, n = 0;
-            int units = 0;
-            for (s = sa;; ++s) {
-                units = att_units(a, s < kAttLens ? lens[s] : att_len(a, s));
-                n = units * per_unit;
-                if (s == sb - 1 || at + n > border) break;
-                at += n;
+        for (int i = 0; i < 2; ++i) {                            // (one thread's sequences hold either border)
+            const int c = (int)blockIdx.x + i;                   // total * c / ctas
+            const long long border = blockIdx.x < ctas ? each * c + (int)(total - each * ctas) * c / (int)ctas : total;
+            if (!(border == total ? tid == 0 : border >= before && border < before + mine)) continue;
+            long long u = total, off = 0;
+            int s = a.c.S;
+            if (border < total) {
+                long long at = before, n = 0;
+                int units = 0;
+                for (s = sa;; ++s) {
+                    units = att_units(a, s < kAttLens ? lens[s] : att_len(a, s));
+                    n = units * per_unit;
+                    if (s == sb - 1 || at + n > border) break;
+                    at += n;
+                }
+                off = snapped(border - at, units);
+                u = at + off;
+                if (off == n) ++s, off = 0;
             }
-            off = border - at;
-            const int in = (int)(off - quotient(off, units) * units);
-            if (in <= kAttPairUnits + kAttSnap) off -= in;
-            else if (in >= units - kAttSnap) off += units - in;
-            u = at + off;
-            if (off == n) ++s, off = 0;
-        }
-        if (few) {
-            const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
-            u = __shfl_sync(0xffffffffu, u, from);
-            if (i == 0) walk.u = u, walk.off = __shfl_sync(0xffffffffu, off, from), walk.seq = __shfl_sync(0xffffffffu, s, from);
-            else walk.u1 = u;
-        } else if (here) {
             s_u[i] = u;
             if (i == 0) s_at = off, s_seq = s;
         }
-    }
-    if (!few) {
         __syncthreads();
         walk.u = s_u[0], walk.u1 = s_u[1], walk.seq = s_seq, walk.off = s_at;
     }
@@ -1021,7 +1037,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             if (!(header & kAttEmpty)) {
                 if (header & kAttTree) {
                     const int row = s_segment[warp].group * 16 * WR + wr * 16 + (lane >> 2);
-                    att_tile<D, F8, WR, HALF, true>(acc, q.f, q_smem, tile, note, scale, min(row, rows - 1) / a.group, min(row + 8, rows - 1) / a.group);
+                    att_tile<D, F8, WR, HALF, true>(acc, q.f, q_smem, tile, note, scale, kv_row_of(a, min(row, rows - 1)), kv_row_of(a, min(row + 8, rows - 1)));
                 } else {
                     att_tile<D, F8, WR, HALF, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
                 }
@@ -1098,12 +1114,12 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         const bool broken = ld_shared(smem_u32(&s_dead)) != 0;
         float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * (D + 2);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < (HALF ? 1 : 2); ++r) {
             float l = acc.l[r];
             l += __shfl_xor_sync(0xffffffffu, l, 1);
             l += __shfl_xor_sync(0xffffffffu, l, 2);
             float m = acc.m[r];
-            const int row = r ? r1 : r0, qi = row / a.group;
+            const int row = r ? r1 : r0, qi = kv_row_of(a, row);
             if (row >= rows) continue;
             const int64_t t = (int64_t)g.seq * a.Q + qi, to = t * a.Hq + g.head * a.group + (row - qi * a.group);
             const bool blind = a.node && ld_cg_s32(a.node + t) < -1;                       // a row of no token
@@ -1218,11 +1234,15 @@ cudaError_t attend_go(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
         if (map_fns().replace(&k_map, a.c.k) != CUDA_SUCCESS || map_fns().replace(&v_map, a.c.v) != CUDA_SUCCESS) return cudaErrorInvalidValue;
     }
     const int64_t rows = (int64_t)a.Q * a.group, groups = (rows + 16 * WR - 1) / (16 * WR);
+    KvAttendArgs args = a;
+    // (units of all sequences at the most, times the CTAs)
+    const double most = (double)a.c.S * a.c.heads * groups * ((kv_capacity(a.c) + kAttUnit - 1) / kAttUnit + kAttPairUnits + kAttTreeUnits) * kKvMaxCtas;
+    args.few = a.c.S <= 32 && most < 2147483647.0;
     int64_t grid = (int64_t)a.c.S * a.c.heads * groups * ((kv_capacity(a.c) + kAttUnit - 1) / kAttUnit);
     if (grid > num_sms()) grid = num_sms();
     if (grid > kKvMaxCtas) grid = kKvMaxCtas;
     ctas = (int)grid;
-    return launch_dependent(kernel, (unsigned)grid, kAttThreads, C::kSmem, s, a, k_map, v_map);
+    return launch_dependent(kernel, (unsigned)grid, kAttThreads, C::kSmem, s, args, k_map, v_map);
 }
 
 template <int D, bool F8>

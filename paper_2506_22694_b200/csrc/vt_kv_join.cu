@@ -84,6 +84,7 @@ size_t kv_attend_scratch_bytes(int rows, int d) {
 void kv_attend_carve(KvAttendArgs& a, uint8_t* scratch) {
     a.meta = reinterpret_cast<int4*>(scratch);
     a.part = reinterpret_cast<float*>(scratch + align_up(kKvMaxCtas * sizeof(int4), 256));
+    a.inv_group = 1.0f / (float)a.group;
     a.page_shift = -1;
     for (int i = 0; i < 31; ++i)
         if (a.c.page == 1 << i) a.page_shift = i;

@@ -55,7 +55,7 @@ __device__ __forceinline__ JoinSum join_sum(const KvAttendArgs& a, int c, int pa
 __device__ __forceinline__ void join_store(const KvAttendArgs& a, int seq, int head, int row, int col, const JoinSum& s) {
     const float4 o = s.o;
     const float l = s.l;
-    const int qi = row / a.group;
+    const int qi = kv_row_of(a, row);
     const int64_t to = ((int64_t)seq * a.Q + qi) * a.Hq + head * a.group + (row - qi * a.group);
     const bool none = l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
