@@ -13,9 +13,10 @@
 // delivers it), and it keeps scores and weights in registers, where tcgen05 would send both through TMEM for tiles of 128 rows that
 // are seven eighths empty.
 //
-// Measured (heads of 128, 8 key heads): 64 sequences of up to 8000 tokens, bf16, 172 us, 92% of what copying HBM reaches; e4m3 106 us, 75%: there the
-// producers' instructions bound it (a tile has half the bytes and the exponents on top).  One sequence of 4001 tokens: 12.6 us, of which 8 are
-// what a call of 64 tokens takes: launch 2.5, lengths 1.6, queries and first page ids 0.9, first tile 1.5, meeting and end 2.
+// Measured (heads of 128, 8 key heads): 64 sequences of up to 8000 tokens, bf16, 172 us, 92% of what copying HBM reaches; e4m3 104 us, 77%: there the
+// producers' instructions bound it (a tile has half the bytes and the exponents on top).  One sequence of 4000 tokens: 14 us, of which 7 are
+// what a call of 64 tokens takes: 1.7 before it starts, lengths and shares 1, page ids and first copies 1.7, a tile 0.8, meeting
+// and results 1.7.  The rest: another tile a team, the fence and the ticket of a part 0.9, the join 1.6.
 //
 // Split: the work is cut into units of 64 tokens, in the order (sequence, key head, group of rows, tokens), and every CTA takes an equal run of
 // units, whatever the lengths are; nothing is known to the host, so a captured graph stays right when lengths change.  A (sequence, head, group)
@@ -44,9 +45,12 @@ constexpr int kAttConsumerRegs = 200, kAttProducerRegs = 104;
 static_assert(kAttWarps * kAttConsumerRegs + kAttFeeds * kAttProducerRegs <= (kAttWarps + kAttFeeds) * 168, "what the block was launched with");
 constexpr int kAttUnit = 64;                                     // tokens
 // What a result counts for besides its tokens when the work is dealt out (the walk to it, its queries, the meeting), and a tree's tokens.
-// 64 ragged sequences of up to 8000 tokens, us with 2 / 4 / 8 / 12 for a result: bf16 186 / 174 / 169 / 170, e4m3 145 / 133 / 115 / 112.
+// 64 ragged sequences of up to 8000 tokens, us with 2 / 4 / 8 / 12 for a result (parts still joined by a second launch): bf16 186 / 174 / 169 / 170,
+// e4m3 145 / 133 / 115 / 112.
 constexpr int kAttPairUnits = 8, kAttTreeUnits = 12;
-constexpr int kAttSnap = 2;                                      // no result is split so near to its ends
+// No result is split so near to its ends.  2 / 4 / 6 / 10: a tree over 4001 tokens 21.7 / 23.1 / 26.2 / 32.3 us, a token over 1024 12.7 / 14.4 /
+// 14.6 / 15.2, batches alike.
+constexpr int kAttSnap = 2;
 constexpr int kAttLens = 1024;                                   // sequences whose lengths are kept in shared memory
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
 constexpr int kAttTurns = 2;                                     // tiles of a producer in a round

@@ -1,4 +1,4 @@
-// Joins the partial results of the paged attention: a (sequence, key head, group of rows) whose tokens lay in several CTAs has one partial
+// Joins the partial results of the paged attention where the attention kernel does not (over eight rows a key head): a (sequence, key head, group of rows) whose tokens lay in several CTAs has one partial
 // result from each, which are added up in the order of the tokens (so that the result does not depend on timing).
 //
 // Latency-bound: a result of 37 parts is 20 KB a row, but a chain of loads for one thread.  The rows of all joined results are dealt out as

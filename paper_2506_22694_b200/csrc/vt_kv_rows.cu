@@ -211,7 +211,8 @@ __device__ __forceinline__ uint2 to_e4m3(const F* x, uint32_t& exp_byte) {
 // ---- write ------------------------------------------------------------------------------------------------------
 // A warp takes a share of one token's heads, 32 / LG heads at a time, queries first, then keys, then values: the token's sines are made
 // once for all of them.  For prompts bound by the memory and, close behind, by instructions (the head size is a constant for their sake);
-// latency-bound for a token: `shares` spreads a few tokens over more warps.
+// latency-bound for a token: `shares` spreads a few tokens over more warps.  8.5k tokens of 48 heads of 128 in bf16 (209 MB) take 49 us, 66%
+// of what copying HBM reaches; the same loads and stores without the arithmetic took 42.  One token: 5 us.
 template <int D>
 struct Rows {
     static constexpr int kLanes = D <= 64 ? 8 : D <= 128 ? 16 : 32, kHeads = 32 / kLanes, kStep = kHeads * D;      // of a pass
@@ -369,7 +370,8 @@ __device__ __forceinline__ uint4 from_e4m3(const uint2& w, float f) {
 }
 
 // A warp a token, two passes (of 32 / LG heads) of its keys and of its values in flight.  HBM-bound, and more warps do better than more rows in
-// flight of each: 122k tokens of eight e4m3 heads of 128 (526 MB) take 112 us with four passes and two CTAs an SM, 99 with two passes and four.
+// flight of each: 122k tokens of eight e4m3 heads of 128 (526 MB) took 112 us with four passes and two CTAs an SM, 99 with two passes and four, and
+// take 92 with a warp a token (87% of what copying HBM reaches).
 template <int LG, bool E4M3>
 __global__ void __launch_bounds__(kThreads, 4)
 k_kv_read(const __grid_constant__ KvReadArgs a) {
@@ -416,7 +418,7 @@ k_kv_read(const __grid_constant__ KvReadArgs a) {
 // ---- commit -----------------------------------------------------------------------------------------------------
 // The accepted nodes' rows move to the places behind the committed tokens: place len + i takes the row at len + node(i).  A path's
 // nodes rise, so node(i) >= i: a place is read before it is written when a thread, which owns the same 16 bytes of every row, reads
-// up to eight rows before it writes them, path in order.  One CTA a sequence; latency-bound.
+// up to eight rows before it writes them, path in order.  One CTA a sequence; latency-bound: 4.3 us for one path, 5.8 for 256.
 constexpr int kCommitChunk = 128;
 __global__ void __launch_bounds__(kThreads)
 k_kv_commit(const __grid_constant__ KvCommitArgs a) {
