@@ -93,9 +93,9 @@ struct AttCfg {
         return vec / kVecs * (kTile * kBox) + row * kBox + ((vec % kVecs ^ swizzle(row)) << 4);
     }
 };
-// What an e4m3 tile holds of a token (bf16: the second alone): the power of two of its key (0: no such token), 0 or (no such token) -inf to be
-// added to its score, the exponent of its values within what keeps all weights finite, and their power of two (0: no such token).
-enum { kAttEnd = 1, kAttEmpty = 2, kAttTree = 4 };               // a tile's header
+// What an e4m3 tile holds of a token (bf16: the second alone): the power of two of its key, whether there is no such token, the exponent of its
+// values within what keeps all weights finite, and their power of two (0: no such token).
+enum { kAttEnd = 1, kAttEmpty = 2, kAttTree = 4, kAttShort = 8 };            // a tile's header (short: some tokens are missing)
 
 // One lane of a converged warp: the compiler then knows that one thread is active.
 __device__ __forceinline__ bool elect_lane() {
@@ -224,9 +224,10 @@ struct AttAcc {
 };
 
 // One tile: scores of the warp's 16 rows with its tokens, running maximum, weighted values.  LIST: tokens are a tree's nodes, and the
-// tile's masks say which new rows see each.  HALF: there are eight rows at the most, the lanes' second rows are none.
+// tile's masks say which new rows see each.  HALF: there are eight rows at the most, the lanes' second rows are none.  `some`: tokens are
+// missing (their keys are zeros, of which an infinite query makes a NaN: the score is replaced, nothing is added to it).  No row sees a missing node.
 template <int D, bool F8, int WR, bool HALF, bool LIST>
-__device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, const uint8_t* slot, const uint8_t* note, const float (&scale)[2],
+__device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4], uint32_t q_smem, const uint8_t* slot, const uint8_t* note, bool some, const float (&scale)[2],
                                          int qi0, int qi1) {
     using C = AttCfg<D, F8, WR>;
     constexpr int NT = C::kTile / 8;                             // groups of 8 tokens
@@ -272,36 +273,48 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
     }
     // scores in base 2; what they stand against (the reference) is their maximum, of e4m3 with the exponent of the token's values on top, so
     // that weight times power of two fits f16 whatever the powers are
-    float top[2] = {-INFINITY, -INFINITY}, vf[NT][2];
+    float top[2] = {-INFINITY, -INFINITY}, ve[NT][2], vf[NT][2];
     uint32_t sees[2] = {0, 0};                                   // LIST: bit 2 i + u: the row sees token 8 i + 2 j + u
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        float ve[2] = {0.0f, 0.0f};
+    for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int t = 8 * i + 2 * j + u;
             if (F8) {
                 // (the powers of the key and of the query first: a large one may undo a small one)
                 const float4 x = *reinterpret_cast<const float4*>(note + 16 * t);
-                s[i][u] = fmaf(s[i][u], x.x * scale[0], x.y);
-                if (!HALF) s[i][2 + u] = fmaf(s[i][2 + u], x.x * scale[1], x.y);
-                ve[u] = x.z, vf[i][u] = x.w;
+                s[i][u] *= x.x * scale[0];
+                if (!HALF) s[i][2 + u] *= x.x * scale[1];
+                ve[i][u] = x.z, vf[i][u] = x.w;
             } else {
-                const float bias = *reinterpret_cast<const float*>(note + 4 * t);
-                s[i][u] = fmaf(s[i][u], scale[0], bias);
-                if (!HALF) s[i][2 + u] = fmaf(s[i][2 + u], scale[1], bias);
+                s[i][u] *= scale[0];
+                if (!HALF) s[i][2 + u] *= scale[1];
             }
+        }
+    if (!LIST && some) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int t = 8 * i + 2 * j + u;
+                if (*reinterpret_cast<const uint32_t*>(note + (F8 ? 16 * t + 4 : 4 * t))) s[i][u] = s[i][2 + u] = -INFINITY;
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
             if (LIST) {
+                const int t = 8 * i + 2 * j + u;
                 const unsigned long long bits = *reinterpret_cast<const unsigned long long*>(note + C::kMasks + 8 * t);
                 const bool r0 = (bits >> qi0) & 1, r1 = (bits >> qi1) & 1;
                 sees[0] |= (uint32_t)r0 << (2 * i + u), sees[1] |= (uint32_t)r1 << (2 * i + u);
                 if (!r0) s[i][u] = -INFINITY;
                 if (!r1) s[i][2 + u] = -INFINITY;
             }
-            top[0] = fmaxf(top[0], s[i][u] + ve[u]);
-            if (!HALF) top[1] = fmaxf(top[1], s[i][2 + u] + ve[u]);
+            top[0] = fmaxf(top[0], F8 ? s[i][u] + ve[i][u] : s[i][u]);
+            if (!HALF) top[1] = fmaxf(top[1], F8 ? s[i][2 + u] + ve[i][u] : s[i][2 + u]);
         }
-    }
     bool grows = false;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -717,23 +730,25 @@ struct AttProducer {
     }
 
     __device__ void note(const AttTokens& r, int turn, uint32_t at, bool some) {
-        if (some) {
-            const bool ok = r.id[turn] >= 0;
-            const uint32_t bias = ok ? 0u : 0xff800000u;
-            if (F8) {
-                const float ve = (float)min(max((int)r.ve[turn] - 127, -100), 112);
-                st_shared(at + 16 * lane, make_uint4(ok ? __float_as_uint(kv_two_to(r.ke[turn])) : 0u, bias, __float_as_uint(ve), ok ? __float_as_uint(kv_two_to(r.ve[turn])) : 0u));
-            } else {
-                st_shared(at + 4 * lane, bias);
-            }
-            if (r.tree) {
-                st_shared(at + C::kMasks + 8 * lane, (uint32_t)r.mask[turn]);
-                st_shared(at + C::kMasks + 8 * lane + 4, (uint32_t)(r.mask[turn] >> 32));
-            }
-        }
         // (a team's last tile of a round is the one of the highest number)
         const bool end = r.last && kAttFeeds * turn + feed >= kAttFeeds * kAttTurns - C::kTeams;
-        if (lane == 0) st_shared(at + C::kHeader, (uint32_t)((end ? kAttEnd : 0) | (some ? 0 : kAttEmpty) | (r.tree ? kAttTree : 0)));
+        uint32_t header = (end ? kAttEnd : 0) | (some ? 0 : kAttEmpty) | (r.tree ? kAttTree : 0);
+        if (some) {
+            const bool ok = r.id[turn] >= 0;
+            if (F8) {
+                const float ve = (float)min(max((int)r.ve[turn] - 127, -100), 112);
+                st_shared(at + 16 * lane, make_uint4(ok ? __float_as_uint(kv_two_to(r.ke[turn])) : 0u, !ok, __float_as_uint(ve), ok ? __float_as_uint(kv_two_to(r.ve[turn])) : 0u));
+            } else {
+                st_shared(at + 4 * lane, !ok);
+            }
+            if (__any_sync(0xffffffffu, !ok)) header |= kAttShort;
+            if (r.tree) {
+                const unsigned long long mask = ok ? r.mask[turn] : 0;       // (no row sees what is not there)
+                st_shared(at + C::kMasks + 8 * lane, (uint32_t)mask);
+                st_shared(at + C::kMasks + 8 * lane + 4, (uint32_t)(mask >> 32));
+            }
+        }
+        if (lane == 0) st_shared(at + C::kHeader, header);
         __syncwarp();
     }
 
@@ -1041,9 +1056,9 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             if (!(header & kAttEmpty)) {
                 if (header & kAttTree) {
                     const int row = s_segment[warp].group * 16 * WR + wr * 16 + (lane >> 2);
-                    att_tile<D, F8, WR, HALF, true>(acc, q.f, q_smem, tile, note, scale, kv_row_of(a, min(row, rows - 1)), kv_row_of(a, min(row + 8, rows - 1)));
+                    att_tile<D, F8, WR, HALF, true>(acc, q.f, q_smem, tile, note, header & kAttShort, scale, kv_row_of(a, min(row, rows - 1)), kv_row_of(a, min(row + 8, rows - 1)));
                 } else {
-                    att_tile<D, F8, WR, HALF, false>(acc, q.f, q_smem, tile, note, scale, 0, 0);
+                    att_tile<D, F8, WR, HALF, false>(acc, q.f, q_smem, tile, note, header & kAttShort, scale, 0, 0);
                 }
             }
             __syncwarp();
