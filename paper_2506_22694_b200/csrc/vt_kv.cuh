@@ -69,11 +69,13 @@ struct KvAttendArgs {
     float scale_log2;             // the scores' scale times log2(e)
     uint16_t* out;                // [S * Q, Hq, d]
     float* lse;                   // [S * Q, Hq], or nullptr
-    float* part;                  // partial results: kKvMaxCtas * 2 * part_rows * (d + 2)
+    float* part;                  // partial results: kKvMaxCtas * 2 * part_rows * kv_part_floats(d)
     int4* meta;                   // [kKvMaxCtas]
     int32_t part_rows;
     Ctrl* ctrl;
 };
+// Of a row of a partial result: its weighted values, the maximum and the sum of its weights, and (e4m3) what the values stand against.
+__host__ __device__ constexpr int kv_part_floats(int d) { return d + 3; }
 int kv_attend_warp_rows(int rows, int d);        // warps side by side over a key head's rows (1, 2 or 4 of 16 rows each)
 // Whether the attention kernel joins its parts itself: up to eight rows.  The CTA whose part arrives last reads them all, 40 KB for four rows and 19
 // parts; a kernel of its own, which deals more rows out to all CTAs, costs 1 to 2 us more for one token (256 tokens 11.7 us for 9.9, 701 13.6

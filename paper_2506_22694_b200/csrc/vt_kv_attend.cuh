@@ -5,7 +5,10 @@
 //   len + node, the row's node and its ancestors
 //
 // One pass with a running maximum; what is kept of a part (maximum m in base 2, sum l, weighted values o) joins with another part by
-// m' = max, l' = l 2^(m - m') + ..., o' likewise.
+// m' = max, l' = l 2^(m - m') + ..., o' likewise.  Over e4m3 rows o has a maximum of its own, of score plus the exponent e of the token's values:
+// a weight enters the product as 2^(score + e - v), which fits f16 whatever the powers are, l stands against m, and
+// out = o 2^(v - m) / l.  (With one maximum for both, tokens whose scores are as large but whose values are 2^126 times as small as others' fell
+// out of l.)
 //
 // Bound: HBM, 2 * d * (2 or 1) bytes of a token and key head, each read once for all rows that share the head.  So the rows of a key head
 // (its query heads times the sequence's new rows) lie side by side as the 16 rows of an MMA, up to four such groups (WR) on warps that share
@@ -67,14 +70,15 @@ struct AttCfg {
     static constexpr int kBox = kRow % 128 == 0 ? 128 : kRow % 64 == 0 ? 64 : 32;
     static constexpr int kHalf = kTile * kRow;
     static constexpr int kSlot = 2 * kHalf;                      // keys, values
-    static constexpr int kToken = F8 ? 16 : 4;                   // what a tile holds of a token besides its rows
+    static constexpr int kToken = F8 ? 8 : 4;                    // what a tile holds of a token besides its rows
     static constexpr int kMasks = kTile * kToken;                // the rows that see a tree's token, 8 bytes each
     static constexpr int kHeader = kMasks + kTile * 8;
     static constexpr int kNote = kHeader + 16;
     static constexpr bool kQRegs = D <= 128;                     // query fragments stay in registers
     static constexpr int kQPitch = 2 * D + 16;
     static constexpr int kQBytes = kQRegs ? 0 : WR * 16 * kQPitch;
-    static constexpr int kMeet = kAttWarps / 2 * (D / 8 + 1) * 512;   // where the teams' results meet: D / 8 + 1 vectors of each lane of half of them
+    static constexpr int kVectors = D / 8 + (F8 ? 2 : 1);        // of a lane's share of a result
+    static constexpr int kMeet = kAttWarps / 2 * kVectors * 512; // where the teams' results meet: those of half of them
     static constexpr int kParents = 2 * kKvMaxNodes + 4 * kAttLens;                        // ... and the lengths
     static constexpr int kFree = 226 * 1024 - 2048 - kQBytes - kMeet - kParents;
     // A ring of kPer places for each producer.  Tile 4 t + p of a round is producer p's in turn t, and goes to team (4 t + p) mod teams; a place is
@@ -93,8 +97,8 @@ struct AttCfg {
         return vec / kVecs * (kTile * kBox) + row * kBox + ((vec % kVecs ^ swizzle(row)) << 4);
     }
 };
-// What an e4m3 tile holds of a token (bf16: the second alone): the power of two of its key, whether there is no such token, the exponent of its
-// values within what keeps all weights finite, and their power of two (0: no such token).
+// What a tile holds of a token: e4m3: the power of two of its key (0: no such token) and the exponent of its values (NaN: they are no numbers);
+// bf16: whether there is no such token.
 enum { kAttEnd = 1, kAttEmpty = 2, kAttTree = 4, kAttShort = 8 };            // a tile's header (short: some tokens are missing)
 
 // One lane of a converged warp: the compiler then knows that one thread is active.
@@ -214,11 +218,12 @@ __device__ __forceinline__ void att_wait(uint32_t bar, uint32_t parity, uint32_t
 template <int D>
 struct AttAcc {
     float o[D / 8][4];
-    float m[2], l[2];             // e4m3: m is the maximum of score plus the values' exponent
+    float m[2], l[2];
+    float v[2];                   // e4m3: what o stands against, the maximum of score plus the values' exponent
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-        m[0] = m[1] = -INFINITY;
+        m[0] = m[1] = v[0] = v[1] = -INFINITY;
         l[0] = l[1] = 0.0f;
     }
 };
@@ -271,9 +276,8 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
             }
         }
     }
-    // scores in base 2; what they stand against (the reference) is their maximum, of e4m3 with the exponent of the token's values on top, so
-    // that weight times power of two fits f16 whatever the powers are
-    float top[2] = {-INFINITY, -INFINITY}, ve[NT][2], vf[NT][2];
+    // scores in base 2, and their maxima (e4m3: with the exponent of the values on top, too)
+    float top[2] = {-INFINITY, -INFINITY}, vtop[2] = {-INFINITY, -INFINITY}, ve[NT][2];
     uint32_t sees[2] = {0, 0};                                   // LIST: bit 2 i + u: the row sees token 8 i + 2 j + u
 #pragma unroll
     for (int i = 0; i < NT; ++i)
@@ -282,10 +286,10 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
             const int t = 8 * i + 2 * j + u;
             if (F8) {
                 // (the powers of the key and of the query first: a large one may undo a small one)
-                const float4 x = *reinterpret_cast<const float4*>(note + 16 * t);
+                const float2 x = *reinterpret_cast<const float2*>(note + 8 * t);
                 s[i][u] *= x.x * scale[0];
                 if (!HALF) s[i][2 + u] *= x.x * scale[1];
-                ve[i][u] = x.z, vf[i][u] = x.w;
+                ve[i][u] = x.y;
             } else {
                 s[i][u] *= scale[0];
                 if (!HALF) s[i][2 + u] *= scale[1];
@@ -296,8 +300,8 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
         for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int t = 8 * i + 2 * j + u;
-                if (*reinterpret_cast<const uint32_t*>(note + (F8 ? 16 * t + 4 : 4 * t))) s[i][u] = s[i][2 + u] = -INFINITY;
+                const uint32_t x = *reinterpret_cast<const uint32_t*>(note + C::kToken * (8 * i + 2 * j + u));
+                if (F8 ? !x : x) s[i][u] = s[i][2 + u] = -INFINITY;
             }
     }
 #pragma unroll
@@ -312,45 +316,48 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                 if (!r0) s[i][u] = -INFINITY;
                 if (!r1) s[i][2 + u] = -INFINITY;
             }
-            top[0] = fmaxf(top[0], F8 ? s[i][u] + ve[i][u] : s[i][u]);
-            if (!HALF) top[1] = fmaxf(top[1], F8 ? s[i][2 + u] + ve[i][u] : s[i][2 + u]);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                top[r] = fmaxf(top[r], s[i][2 * r + u]);
+                if (F8) vtop[r] = fmaxf(vtop[r], s[i][2 * r + u] + ve[i][u]);
+            }
         }
+    // (a row's maximum is that of its four lanes; whether it grows, any of them can say)
     bool grows = false;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-        grows |= top[r] > acc.m[r] + 4.0f;
-    }
-    // The kept reference may lie up to 4 below the true one (weights up to 16): results are divided by the sum of the same weights,
+    for (int r = 0; r < NR; ++r) grows |= top[r] > acc.m[r] + 4.0f || (F8 && vtop[r] > acc.v[r] + 4.0f);
+    // The kept references may lie up to 4 below the true ones (weights up to 16): results are divided by the sum of the same weights,
     // and most tiles need not scale what is there.
     if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const float m = fmaxf(acc.m[r], top[r]);
+#pragma unroll
+            for (int o = 1; o < 4; o *= 2) {
+                top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], o));
+                if (F8) vtop[r] = fmaxf(vtop[r], __shfl_xor_sync(0xffffffffu, vtop[r], o));
+            }
+            const float m = fmaxf(acc.m[r], top[r]), v = fmaxf(acc.v[r], vtop[r]);
             const float f = m == acc.m[r] ? 1.0f : exp2_fast(acc.m[r] - m);
-            acc.m[r] = m;
+            const float g = !F8 ? f : v == acc.v[r] ? 1.0f : exp2_fast(acc.v[r] - v);
+            acc.m[r] = m, acc.v[r] = v;
             acc.l[r] *= f;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) acc.o[i][2 * r] *= f, acc.o[i][2 * r + 1] *= f;
+            for (int i = 0; i < D / 8; ++i) acc.o[i][2 * r] *= g, acc.o[i][2 * r + 1] *= g;
         }
     }
-    const float m0 = acc.m[0] == -INFINITY ? 0.0f : acc.m[0], m1 = acc.m[1] == -INFINITY ? 0.0f : acc.m[1];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        s[i][0] = exp2_fast(s[i][0] - m0), s[i][1] = exp2_fast(s[i][1] - m0);
-        acc.l[0] += s[i][0] + s[i][1];
-        if (!HALF) {
-            s[i][2] = exp2_fast(s[i][2] - m1), s[i][3] = exp2_fast(s[i][3] - m1);
-            acc.l[1] += s[i][2] + s[i][3];
-        }
-        if (F8) {
-            s[i][0] *= vf[i][0], s[i][1] *= vf[i][1];
-            if (!HALF) s[i][2] *= vf[i][0], s[i][3] *= vf[i][1];
-            if (LIST) {                                          // (a power of a row that held a NaN is one)
+    for (int r = 0; r < NR; ++r) {
+        const float m = acc.m[r] == -INFINITY ? 0.0f : acc.m[r], v = acc.v[r] == -INFINITY ? 0.0f : acc.v[r];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (!((sees[u >> 1] >> (2 * i + (u & 1))) & 1)) s[i][u] = 0.0f;
+        for (int i = 0; i < NT; ++i) {
+            const float p0 = exp2_fast(s[i][2 * r] - m), p1 = exp2_fast(s[i][2 * r + 1] - m);
+            acc.l[r] += p0 + p1;
+            s[i][2 * r] = F8 ? exp2_fast(s[i][2 * r] + ve[i][0] - v) : p0;
+            s[i][2 * r + 1] = F8 ? exp2_fast(s[i][2 * r + 1] + ve[i][1] - v) : p1;
+            if (F8 && LIST) {                                    // (the exponent of a row that held a NaN is one)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (!((sees[r] >> (2 * i + u)) & 1)) s[i][2 * r + u] = 0.0f;
             }
         }
     }
@@ -736,8 +743,9 @@ struct AttProducer {
         if (some) {
             const bool ok = r.id[turn] >= 0;
             if (F8) {
-                const float ve = (float)min(max((int)r.ve[turn] - 127, -100), 112);
-                st_shared(at + 16 * lane, make_uint4(ok ? __float_as_uint(kv_two_to(r.ke[turn])) : 0u, !ok, __float_as_uint(ve), ok ? __float_as_uint(kv_two_to(r.ve[turn])) : 0u));
+                const float ve = r.ve[turn] == 255 ? NAN : (float)((int)r.ve[turn] - 127);
+                st_shared(at + 8 * lane, ok ? __float_as_uint(kv_two_to(r.ke[turn])) : 0u);
+                st_shared(at + 8 * lane + 4, __float_as_uint(ok ? ve : 0.0f));
             } else {
                 st_shared(at + 4 * lane, !ok);
             }
@@ -1089,31 +1097,33 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         // (of a short segment's teams only the first have had tokens)
         const int active = min((max(g.token_end - g.token, g.tree ? a.N : 0) + C::kTile - 1) / C::kTile, C::kTeams);
         if (active > 1 || !C::kQRegs) consumers_barrier();       // (the meeting place is free, and so are the queries' rows)
-        constexpr int kShare = D / 8 + 1;                        // vectors of a lane
         bool first_step = true;
 #pragma unroll
         for (int half = C::kTeams / 2; half >= 1; half /= 2) {
             if (half >= active) continue;
             // who gives uses the place that it has read from: its own place, or in the first step that of the reader
-            float4* place = meet + (team >= half && first_step ? warp - half * WR : warp) * kShare * 32 + lane;
+            float4* place = meet + (team >= half && first_step ? warp - half * WR : warp) * C::kVectors * 32 + lane;
             if (team >= half && team < 2 * half) {
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) place[32 * i] = make_float4(acc.o[i][0], acc.o[i][1], acc.o[i][2], acc.o[i][3]);
                 place[32 * (D / 8)] = make_float4(acc.m[0], acc.m[1], acc.l[0], acc.l[1]);
+                if (F8) place[32 * (D / 8 + 1)] = make_float4(acc.v[0], acc.v[1], 0.0f, 0.0f);
             }
             consumers_barrier();
             if (team < half) {
-                const float4* from = first_step ? place : place + half * WR * kShare * 32;
+                const float4* from = first_step ? place : place + half * WR * C::kVectors * 32;
                 const float4 y = from[32 * (D / 8)];
                 const float ym[2] = {y.x, y.y}, yl[2] = {y.z, y.w};
-                float fa[2], fb[2];
+                float fa[2], fb[2], yv[2] = {-INFINITY, -INFINITY};
+                if (F8) yv[0] = from[32 * (D / 8 + 1)].x, yv[1] = from[32 * (D / 8 + 1)].y;
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const float m = fmaxf(acc.m[r], ym[r]);
-                    fa[r] = acc.m[r] == -INFINITY ? 1.0f : exp2_fast(acc.m[r] - m);   // (a part of no token: nothing to scale)
-                    fb[r] = ym[r] == -INFINITY ? 1.0f : exp2_fast(ym[r] - m);
+                    const float m = fmaxf(acc.m[r], ym[r]), v = fmaxf(acc.v[r], yv[r]);
+                    fa[r] = part_weight(acc.m[r], m), fb[r] = part_weight(ym[r], m);
                     acc.m[r] = m;
                     acc.l[r] = acc.l[r] * fa[r] + yl[r] * fb[r];
+                    if (F8) fa[r] = part_weight(acc.v[r], v), fb[r] = part_weight(yv[r], v);
+                    acc.v[r] = v;
                 }
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) {
@@ -1131,7 +1141,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         if (!HALF && !whole && g.tile0 == 0) meta = make_int4(last_cta, g.seq, g.head, g.group);
         if (team != 0) continue;
         const bool broken = ld_shared(smem_u32(&s_dead)) != 0;
-        float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * (D + 2);
+        float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * kv_part_floats(D);
 #pragma unroll
         for (int r = 0; r < (HALF ? 1 : 2); ++r) {
             float l = acc.l[r];
@@ -1145,12 +1155,13 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
             if (broken) l = NAN;
             const bool none = blind || l == 0.0f;
             if (blind) m = -INFINITY, l = 0.0f;
-            const float inv = whole ? 1.0f / l : 1.0f;
+            const float inv = whole ? 1.0f / l : 1.0f, power = F8 && whole ? exp2_fast(0.5f * (acc.v[r] - m)) : 1.0f;
             const int lr = row - row0;
             if (whole) {
                 if (j == 0 && a.lse) a.lse[to] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
             } else if (j == 0) {
                 part[a.part_rows * D + lr] = m, part[a.part_rows * (D + 1) + lr] = l;
+                if (F8) part[a.part_rows * (D + 2) + lr] = blind ? -INFINITY : acc.v[r];
             }
 #pragma unroll
             for (int i = 0; i < D / 8; i += F8 ? 2 : 1) {
@@ -1158,7 +1169,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
                 if (F8) x[0] = acc.o[i][2 * r], x[1] = acc.o[i + 1][2 * r], x[2] = acc.o[i][2 * r + 1], x[3] = acc.o[i + 1][2 * r + 1];
                 else x[0] = acc.o[i][2 * r], x[1] = acc.o[i][2 * r + 1], x[2] = x[3] = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : x[e] * inv;
+                for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : F8 ? x[e] * inv * power * power : x[e] * inv;       // (the power in halves: the result fits, it may not)
                 const int d0 = F8 ? 8 * i + 4 * j : 8 * i + 2 * j;
                 if (whole && F8) *reinterpret_cast<uint2*>(a.out + to * D + d0) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
                 else if (whole) *reinterpret_cast<uint32_t*>(a.out + to * D + d0) = pack_bf16(x[0], x[1]);
@@ -1187,6 +1198,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     consumers_barrier();
     constexpr int kVecs = D / 4, kSeats = 32 * kAttWarps / kVecs;
     float* sums = reinterpret_cast<float*>(meet + 32 * kAttWarps);
+    static_assert(32 * kAttWarps * 28 <= C::kMeet, "seven numbers of a thread");
     for (int k = 0; k < 2; ++k) {
         const int4 to = s_join[k];
         if (to.x < 0) continue;
@@ -1195,13 +1207,17 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         for (int r0 = 0; r0 < rows; r0 += at_once) {
             const int row = r0 + which, turn = seat - which * share;
             const bool live = which < at_once && row < rows;
-            JoinSum sum{make_float4(0, 0, 0, 0), -INFINITY, 0.0f};
-            if (live) sum = join_sum(a, to.x, to.y, row, col, turn, share);
+            JoinSum<F8> sum;
+            if (live) sum = join_sum<F8>(a, to.x, to.y, row, col, turn, share);
             meet[tid] = sum.o, sums[tid] = sum.m, sums[32 * kAttWarps + tid] = sum.l;
+            if (F8) sums[64 * kAttWarps + tid] = sum.v;
             consumers_barrier();
             if (live && turn == 0) {
-                for (int i = 1; i < share; ++i) join_add(sum, sums[tid + i * kVecs], sums[32 * kAttWarps + tid + i * kVecs], meet[tid + i * kVecs]);
-                join_store(a, to.z, to.w, row, col, sum);
+                for (int i = 1; i < share; ++i) {
+                    const int x = tid + i * kVecs;
+                    sum.add(JoinSum<F8>{meet[x], sums[x], sums[32 * kAttWarps + x], F8 ? sums[64 * kAttWarps + x] : -INFINITY});
+                }
+                join_store<F8>(a, to.z, to.w, row, col, sum);
             }
             consumers_barrier();                                 // (the sums have been read)
         }

@@ -12,12 +12,13 @@ namespace {
 constexpr int kThreads = 256;
 
 // A thread has four dims of a row and every `share`-th part.
+template <bool F8>
 __global__ void __launch_bounds__(kThreads)
 k_kv_join(const __grid_constant__ KvAttendArgs a, int warp_rows, int ctas) {
     __shared__ int s_first[kKvMaxCtas];                          // CTA with the first part of each joined result, in order
     __shared__ int s_count[kThreads / 32];
     __shared__ float4 s_o[kThreads];
-    __shared__ float s_m[kThreads], s_l[kThreads];
+    __shared__ float s_m[kThreads], s_l[kThreads], s_v[F8 ? kThreads : 1];
     griddep_launch_dependents();
     griddep_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -57,13 +58,17 @@ k_kv_join(const __grid_constant__ KvAttendArgs a, int warp_rows, int ctas) {
         const int last = ld_cg_s32(&a.meta[c].x), seq = ld_cg_s32(&a.meta[c].y), head = ld_cg_s32(&a.meta[c].z), group = ld_cg_s32(&a.meta[c].w);
         const int row = group * 16 * warp_rows + lr, parts = last - c + 1;
         const bool live = which < at_once && t < min(tasks, ((int)blockIdx.x + 1) * each) && row < a.Q * a.group;
-        JoinSum s{make_float4(0, 0, 0, 0), -INFINITY, 0.0f};
-        if (live) s = join_sum(a, c, parts, lr, col, turn, share);
+        JoinSum<F8> s;
+        if (live) s = join_sum<F8>(a, c, parts, lr, col, turn, share);
         s_o[tid] = s.o, s_m[tid] = s.m, s_l[tid] = s.l;
+        if (F8) s_v[tid] = s.v;
         __syncthreads();
         if (live && turn == 0) {
-            for (int i = 1; i < share; ++i) join_add(s, s_m[tid + i * vecs], s_l[tid + i * vecs], s_o[tid + i * vecs]);
-            join_store(a, seq, head, row, col, s);
+            for (int i = 1; i < share; ++i) {
+                const int x = tid + i * vecs;
+                s.add(JoinSum<F8>{s_o[x], s_m[x], s_l[x], F8 ? s_v[x] : -INFINITY});
+            }
+            join_store<F8>(a, seq, head, row, col, s);
         }
         __syncthreads();                                         // (the sums have been read)
     }
@@ -77,7 +82,7 @@ int kv_attend_warp_rows(int rows, int d) { return d > 128 ? 2 : rows <= 16 ? 1 :
 static int part_rows(int rows, int d) { return rows < 16 * kv_attend_warp_rows(rows, d) ? rows : 16 * kv_attend_warp_rows(rows, d); }
 
 size_t kv_attend_scratch_bytes(int rows, int d) {
-    const size_t parts = (size_t)kKvMaxCtas * 2 * ((part_rows(rows, d) + 3) & ~3) * (d + 2) * sizeof(float);
+    const size_t parts = (size_t)kKvMaxCtas * 2 * ((part_rows(rows, d) + 3) & ~3) * kv_part_floats(d) * sizeof(float);
     return align_up(kKvMaxCtas * sizeof(int4), 256) + parts;
 }
 
@@ -99,7 +104,7 @@ cudaError_t launch_kv_attend(const KvAttendArgs& a, cudaStream_t s) {
     if (kv_attend_joins(a.Q * a.group, a.c.d)) return cudaSuccess;
     const int wr = kv_attend_warp_rows(a.Q * a.group, a.c.d);
     const unsigned grid = (unsigned)(2 * num_sms());
-    return launch_dependent(k_kv_join, grid, kThreads, 0, s, a, wr, ctas);
+    return launch_dependent(a.c.k_exp ? k_kv_join<true> : k_kv_join<false>, grid, kThreads, 0, s, a, wr, ctas);
 }
 
 }  // namespace vt

@@ -1,4 +1,4 @@
-"""Attention over the paged cache where numbers go to their ends: infinite queries beside missing tokens."""
+"""Attention over the paged cache where numbers go to their ends: infinite queries beside missing tokens, powers of values that lie far apart."""
 import math
 
 import pytest
@@ -36,3 +36,33 @@ def test_an_infinite_query_is_not_multiplied_with_what_is_missing(d, Hq, page, e
     first = host.k.view(torch.uint8)[..., 0] if e4m3 else host.k[..., 0]
     first.copy_(torch.full_like(first, 0x38) if e4m3 else torch.ones_like(first))
     check(host, q, lens, 1, node)
+
+
+@pytest.mark.parametrize("power", [40, 100, -80])
+@pytest.mark.parametrize("d,Hq,Q", [(64, 2, 1), (64, 8, 2), (128, 4, 1), (128, 32, 2), (128, 16, 4), (256, 2, 1), (256, 20, 1)])
+def test_powers_of_values_that_lie_far_apart(d, Hq, Q, power):
+    """Rows of zeros (their power is 2^-126) in front of, behind and between rows of 2^power: a token counts in the sum of weights by its
+    score alone.  In one tile, in tiles of several teams and in parts of several CTAs."""
+    for n in (32, 64, 65, 300, 3000):
+        for order in ("front", "behind", "between", "teams"):
+            host = ku.Host(1, n + 8, 1, d, 16, True, seed=n)
+            host.ve = torch.full_like(host.ve, 127 + power - 6)
+            none = {"front": lambda i: i < n // 2, "behind": lambda i: i >= n // 2, "between": lambda i: i % 2, "teams": lambda i: i // 32 % 2}[order]
+            for i in range(n + 8):
+                p, j = host.place(0, i)
+                if none(i):
+                    host.v.view(torch.uint8)[p, :, j], host.ve[p, :, j] = 0, 1
+            node = torch.arange(Q, dtype=I32) + 3 if Q > 1 else None
+            check(host, ku.bf16((Q, Hq, d), 3), [n], Q, node)
+
+
+def test_written_rows_of_zeros_count_as_tokens():
+    """As a program meets them: rows of zeros and rows of 2^40 through the write, equal scores."""
+    cache, pages = vt.kv_cache(5, 1, 16, 64, e4m3=True), torch.arange(4, dtype=I32, device="cuda")[None]
+    k = torch.zeros((64, 1, 64), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    v[32:] = 2.0 ** 40
+    at = torch.arange(64, dtype=I32, device="cuda")
+    q = vt.vt_qkv_write(torch.ones((64, 1, 64), dtype=torch.bfloat16, device="cuda"), k, v, cache, pages, at)
+    out, lse = vt.vt_kv_attend(q[:1], cache, pages, at[:1] + 64)
+    assert bool((out == 2.0 ** 39).all()) and abs(float(lse) - math.log(64)) < 1e-5
