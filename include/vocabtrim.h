@@ -413,7 +413,8 @@ vt_status vt_kv_read(const vt_kv_cache *cache, const int32_t *seq, const int32_t
  *   out [S*Q,Hq,d] bf16; lse [S*Q,Hq] fp32 or NULL.  A row whose weights sum to zero (it sees no token, or scores of -inf) has
  *     zeros and an lse of -inf.
  * Sums, maxima and scores are fp32; weights enter the products as two bf16 pieces (what is lost is 2^-17 of one), over an
- * e4m3 cache as one f16 number (2^-11).  out must not overlap q or the cache.  Sequences may have any lengths;
+ * e4m3 cache, times the power of the token's values, as one f16 number (2^-11 of it, or 2^-36 of the row's largest such
+ * product where that is more).  out must not overlap q or the cache.  Sequences may have any lengths;
  * results are the same from call to call.  Workspace: vt_workspace_bytes(VT_OP_KV_ATTEND, ...).
  */
 vt_status vt_kv_attend(const uint16_t *q, int64_t q_ld, int32_t Q, int32_t Hq, const vt_kv_cache *cache, const int32_t *lens,

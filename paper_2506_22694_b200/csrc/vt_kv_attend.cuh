@@ -54,6 +54,7 @@ constexpr int kAttPairUnits = 8, kAttTreeUnits = 12;
 // No result is split so near to its ends.  2 / 4 / 6 / 10: a tree over 4001 tokens 21.7 / 23.1 / 26.2 / 32.3 us, a token over 1024 12.7 / 14.4 /
 // 14.6 / 15.2, batches alike.
 constexpr int kAttSnap = 2;
+constexpr float kAttLift = 11.0f;                                // e4m3: weights of values are 2^11 to 2^15 at the most, of f16's 65504
 constexpr int kAttLens = 1024;                                   // sequences whose lengths are kept in shared memory
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
 constexpr int kAttTurns = 2;                                     // tiles of a producer in a round
@@ -219,7 +220,7 @@ template <int D>
 struct AttAcc {
     float o[D / 8][4];
     float m[2], l[2];
-    float v[2];                   // e4m3: what o stands against, the maximum of score plus the values' exponent
+    float v[2];                   // e4m3: what o stands against, the maximum of score plus the values' exponent, less kAttLift
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
@@ -325,9 +326,10 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
     // (a row's maximum is that of its four lanes; whether it grows, any of them can say)
     bool grows = false;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) grows |= top[r] > acc.m[r] + 4.0f || (F8 && vtop[r] > acc.v[r] + 4.0f);
+    for (int r = 0; r < NR; ++r) grows |= top[r] > acc.m[r] + 4.0f || (F8 && vtop[r] > acc.v[r] + (4.0f + kAttLift));
     // The kept references may lie up to 4 below the true ones (weights up to 16): results are divided by the sum of the same weights,
-    // and most tiles need not scale what is there.
+    // and most tiles need not scale what is there.  v lies kAttLift below its own: weights up to 2^15 use f16's range, whose numbers lose bits
+    // below 2^-14 and end at 2^-24, as far as it goes.
     if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
@@ -336,7 +338,7 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                 top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], o));
                 if (F8) vtop[r] = fmaxf(vtop[r], __shfl_xor_sync(0xffffffffu, vtop[r], o));
             }
-            const float m = fmaxf(acc.m[r], top[r]), v = fmaxf(acc.v[r], vtop[r]);
+            const float m = fmaxf(acc.m[r], top[r]), v = fmaxf(acc.v[r], vtop[r] - kAttLift);
             const float f = m == acc.m[r] ? 1.0f : exp2_fast(acc.m[r] - m);
             const float g = !F8 ? f : v == acc.v[r] ? 1.0f : exp2_fast(acc.v[r] - v);
             acc.m[r] = m, acc.v[r] = v;
@@ -398,7 +400,8 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
         }
     }
     // bf16: weights go into the MMA as two pieces, the rounded weight and what the rounding left (2^-17 of it at most): one piece alone would
-    // add as much error as the rounding of the result, and at these rates the second MMA is free.  e4m3: one piece of f16 (2^-11).
+    // add as much error as the rounding of the result, and at these rates the second MMA is free.  e4m3: one piece of f16: 2^-11 of a weight, and no
+    // less than 2^-36 of the row's heaviest (which is 2^11 to 2^15 here, and half a step below 2^-14 is 2^-25).
     const uint32_t v_row = ((lane >> 3) & 1) * 8 + (lane & 7), v_at = base + C::kHalf + v_row * C::kBox, v_vec = ((lane >> 4) ^ C::swizzle(v_row)) << 4;
 #pragma unroll
     for (int g = 0; g < C::kTile / 16; ++g) {

@@ -1,4 +1,5 @@
-"""Attention over the paged cache where numbers go to their ends: infinite queries beside missing tokens, powers of values that lie far apart."""
+"""Attention over the paged cache where numbers go to their ends: infinite queries beside missing tokens, powers of values that lie far apart,
+light tokens behind heavy ones."""
 import math
 
 import pytest
@@ -66,3 +67,34 @@ def test_written_rows_of_zeros_count_as_tokens():
     q = vt.vt_qkv_write(torch.ones((64, 1, 64), dtype=torch.bfloat16, device="cuda"), k, v, cache, pages, at)
     out, lse = vt.vt_kv_attend(q[:1], cache, pages, at[:1] + 64)
     assert bool((out == 2.0 ** 39).all()) and abs(float(lse) - math.log(64)) < 1e-5
+
+
+@pytest.mark.parametrize("nats", [8, 15, 16, 17.25, 20])
+@pytest.mark.parametrize("d,Hq", [(64, 2), (64, 32), (128, 1), (128, 40), (256, 2)])
+def test_light_tokens_behind_heavy_ones(d, Hq, nats):
+    """8 tokens e^nats times as heavy as each of the 8184 behind them, one in the first tile of each team, whose values are zero: each of the
+    others is tiny beside them, and the result is theirs.  300 sequences of the same pages, so that a CTA's run holds whole results.  Bound: a
+    weight is off by 2^-11 of it, or by 2^-36 of the heaviest (times power of its values, the same for all here); scores and
+    exponentials by 2^-20; a sum by a step, 2^-23, an addition (fewer than the tokens); out is rounded to bf16."""
+    n, S = 8192, 300
+    host = ku.Host(1, n, 1, d, 64, True, seed=1)
+    host.ke, host.ve = torch.full_like(host.ke, 112), torch.full_like(host.ve, 127 - 7)
+    v = host.v.view(torch.uint8)
+    v &= 0x7f                                                              # all values at least zero
+    scale = nats / (2.0 * d)                                               # queries of one, heavy keys of two
+    for i in range(5, 256, 32):
+        p, j = host.place(0, i)
+        host.k[p, :, j], host.ke[p, :, j] = torch.tensor(2.0).to(torch.float8_e4m3fn), 127
+        host.v.view(torch.uint8)[p, :, j] = 0
+    dev = host.device()
+    out, lse = vt.vt_kv_attend(torch.ones((S, Hq, d), dtype=torch.bfloat16, device="cuda"), dev, host.pages_dev.expand(S, -1).contiguous(),
+                               torch.full((S,), n, dtype=I32, device="cuda"), scale=scale)
+    k, vv = host.values(0, list(range(n)))
+    z = k[:, 0].sum(1) * scale
+    w = torch.softmax(z, 0)
+    ref = (w[:, None] * vv[:, 0]).sum(0)
+    steps = n * 2.0 ** -23
+    tol = (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -20 + 2 * steps + 2.0 ** -19) * ref + n * 2.0 ** -36 * 448 * 2.0 ** -7 * float(w.max())
+    off = (out.double().cpu() - ref).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
+    assert float((lse.double().cpu() - torch.logsumexp(z, 0)).abs().max()) <= 2.0 ** -19 + steps + 2.0 ** -22 * 30
