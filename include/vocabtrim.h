@@ -341,7 +341,7 @@ vt_status vt_draft_head_host(const uint16_t *h_host, const uint16_t *W_trim, con
  *   k_exp, v_exp  VT_KV_E4M3: DEVICE uint8 [n_pages, heads, page], contiguous, 16-byte aligned.  A row stands
  *                 for its e4m3 values times 2^(exp - 127), the smallest power that brings its largest
  *                 magnitude to at most 448 (2^-126 at the least).  255: the row held a NaN or an infinity and
- *                 reads as NaN.  The bytes 0x7f and 0xff are not written.  VT_KV_BF16: NULL.
+ *                 reads as NaN.  The bytes 0x7f and 0xff are not written, and read as NaN.  VT_KV_BF16: NULL.
  *   pages         DEVICE int32 [S, max_pages], rows pages_ld >= max_pages apart; max_pages * page < 2^31.
  *
  * Sequences, places, pages and nodes out of range are left out (not written, not seen, read as zeros) and

@@ -164,6 +164,21 @@ __device__ __forceinline__ void e4m3_pairs(uint32_t x, uint32_t& lo, uint32_t& h
     }
 }
 
+// The tokens of half a tile that hold a byte 0x7f or 0xff (NaN), a bit each.
+template <class C>
+__device__ __forceinline__ uint32_t nan_tokens(const uint8_t* half, int lane) {
+    constexpr int V = C::kRow / 16;
+    uint32_t bad = 0;
+#pragma unroll 4
+    for (int x = lane; x < C::kTile * V; x += 32) {
+        const uint4 w = *reinterpret_cast<const uint4*>(half + C::place(x / V, x % V));
+        uint32_t high = 0;
+        for (const uint32_t y : {w.x, w.y, w.z, w.w}) high |= (y & 0x7f7f7f7fu) + 0x01010101u;
+        if (high & 0x80808080u) bad |= 1u << x / V;
+    }
+    return __reduce_or_sync(0xffffffffu, bad);
+}
+
 // 2^k by its bits, k clamped to what fp32 holds
 __device__ __forceinline__ float two_to(int k) { return __uint_as_float((uint32_t)(min(max(k, -126), 127) + 127) << 23); }
 
@@ -305,6 +320,16 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                 if (F8 ? !x : x) s[i][u] = s[i][2 + u] = -INFINITY;
             }
     }
+    if (F8 && LIST) {                                            // (a NaN went through the product as a number: it is one for the rows that see it)
+        const uint32_t bad = nan_tokens<C>(slot, lane);
+        if (bad) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (bad >> (8 * i + 2 * j + u) & 1) s[i][u] = s[i][2 + u] = NAN;
+        }
+    }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -360,6 +385,24 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
                     if (!((sees[r] >> (2 * i + u)) & 1)) s[i][2 * r + u] = 0.0f;
+            }
+        }
+    }
+    if (F8 && LIST) {
+        const uint8_t* vals = slot + C::kHalf;
+#pragma unroll 1
+        for (uint32_t bad = nan_tokens<C>(vals, lane); bad; bad &= bad - 1) {
+            const int t = __ffs(bad) - 1;
+            const unsigned long long bits = *reinterpret_cast<const unsigned long long*>(note + C::kMasks + 8 * t);
+#pragma unroll
+            for (int i = 0; i < D / 8; i += 2) {                 // (the lane's four dims of every 16)
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vals + C::place(t, i / 2) + 4 * j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if ((w >> (8 * e) & 0x7f) != 0x7f) continue;
+                    if ((bits >> qi0) & 1) acc.o[i + (e & 1)][e >> 1] = NAN;
+                    if ((bits >> qi1) & 1) acc.o[i + (e & 1)][2 + (e >> 1)] = NAN;
+                }
             }
         }
     }

@@ -1,5 +1,5 @@
 """Attention over the paged cache where numbers go to their ends: infinite queries beside missing tokens, powers of values that lie far apart,
-light tokens behind heavy ones."""
+light tokens behind heavy ones, bytes that are no number."""
 import math
 
 import pytest
@@ -98,3 +98,30 @@ def test_light_tokens_behind_heavy_ones(d, Hq, nats):
     off = (out.double().cpu() - ref).abs()
     assert bool((off <= tol).all()), float((off / tol).max())
     assert float((lse.double().cpu() - torch.logsumexp(z, 0)).abs().max()) <= 2.0 ** -19 + steps + 2.0 ** -22 * 30
+
+
+def test_bytes_that_are_no_number():
+    """0x7f and 0xff, which the write never makes, read as NaN wherever they lie: in a committed token, and in a drafted one for the rows
+    that see it, a key's for all dims, a value's for its own."""
+    for Hq, Q, d in ((4, 4, 64), (32, 5, 128), (8, 5, 256), (1, 4, 128)):
+        for what in ("k", "v"):
+            for byte in (0x7f, 0xff):
+                for place in (3, 21 + 0):                                  # committed; node 0, which rows of nodes 4 and 2 see
+                    host = ku.Host(1, 60, 1, d, 16, True, seed=11)
+                    parent = torch.tensor([[-1, -1, 0, 1, 2, 3]], dtype=I32)
+                    node = torch.tensor([4, 5, 2, 3, -1][:Q], dtype=I32)
+                    q = ku.bf16((Q, Hq, d), 3)
+                    p, j = host.place(0, place)
+                    x = host.k if what == "k" else host.v
+                    x.view(torch.uint8)[p, 0, j, 37] = 0
+                    ref, ref_l, tol, tol_l = ku.attend(host, q, [21], Q, node, parent)
+                    sees = torch.ones(Q, dtype=torch.bool) if place == 3 else torch.tensor([True, False, True, False, False][:Q])
+                    if what == "k":
+                        ref[sees], ref_l[sees] = math.nan, math.nan
+                    else:
+                        ref[sees, :, 37] = math.nan
+                    x.view(torch.uint8)[p, 0, j, 37] = byte
+                    out, lse = vt.vt_kv_attend(q.cuda(), host.device(), host.pages_dev, torch.tensor([21], dtype=I32).cuda(), node.cuda(), parent.cuda())
+                    assert ku.near(out, ref, tol)[0] and ku.near(lse, ref_l, tol_l)[0], (Hq, Q, d, what, byte, place)
+                    k, v = vt.vt_kv_read(host.dev, host.pages_dev, torch.tensor([place], dtype=I32).cuda())
+                    assert bool(torch.isnan((k if what == "k" else v)[0, 0, 37]))
