@@ -84,9 +84,10 @@ vt_status vt_workspace_init(void *ws, size_t ws_bytes, void *stream);
 
 /* Every wait inside the kernels (for a bulk copy to land, for another warp's hand-over) is bounded;
  * when a bound expires the kernel stops waiting, lets its own copies land, raises VT_FLAG_TIMEOUT and,
- * for vt_draft_head, reports every row as id -1 / logprob NaN.  This call sets the bound used by the
- * streaming head kernel of calls that take `ws`: `nanoseconds` of device time per wait, 0 = the
- * built-in default (2 s).  The value stays until changed (vt_workspace_init resets it to 0).
+ * for vt_draft_head, reports every row as id -1 / logprob NaN; vt_kv_attend reports the rows that are not
+ * whole as NaN (out and lse).  This call sets the bound used by the streaming head kernel and by
+ * vt_kv_attend in calls that take `ws`: `nanoseconds` of device time per wait, 0 = the
+ * built-in default (2 s), which the other kernels always use.  The value stays until changed (vt_workspace_init resets it to 0).
  * Synchronises `stream`.  (No counterpart in the paper: failure handling of this library.) */
 vt_status vt_workspace_set_wait_limit(void *ws, uint64_t nanoseconds, void *stream);
 

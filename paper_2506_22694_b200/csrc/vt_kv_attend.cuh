@@ -59,7 +59,7 @@ constexpr int kAttLens = 1024;                                   // sequences wh
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
 constexpr int kAttTurns = 2;                                     // tiles of a producer in a round
 constexpr int kAttRound = kAttTile * kAttFeeds * kAttTurns;      // tokens that the producers look up at a time
-constexpr unsigned long long kAttWaitNs = 2000000000ull;         // bound of a wait on a tile or a place in the ring
+constexpr unsigned long long kAttWaitNs = 2000000000ull;         // bound of a wait where the workspace has none, and of copies in flight at the end
 
 template <int D, bool F8, int WR>
 struct AttCfg {
@@ -201,6 +201,12 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
+// (without parking the thread)
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {       // without arriving
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -215,17 +221,30 @@ __device__ __forceinline__ uint32_t ld_shared(uint32_t at) {
     return x;
 }
 
-// A wait within the CTA (nothing here waits for another).  Where it runs out, the flag makes all later waits return at once, every loop still
-// ends, and the results are no numbers.
-__device__ __forceinline__ void att_wait(uint32_t bar, uint32_t parity, uint32_t dead, Ctrl* ctrl) {
-    if (bar_try(bar, parity)) return;
-    const unsigned long long t0 = global_ns();
-    while (!bar_try(bar, parity)) {
-        if (ld_shared(dead)) return;
-        if (global_ns() - t0 > kAttWaitNs) {
-            st_shared(dead, 1u);
+// What bounds a CTA's waits, in shared memory.  The bound is kept with the SM's cycle counter, two cycles a nanosecond: at least the time asked
+// for at any clock up to 2 GHz.  Bounds under a millisecond spin on probes that do not park the thread.
+struct __align__(16) AttStop {
+    long long cycles;
+    long long dead;               // a wait has run out
+};
+constexpr long long kAttShortWait = 2000000;
+__device__ __forceinline__ long long bound_cycles(unsigned long long ns) { return (long long)(ns < (1ull << 61) ? 2 * ns : (1ull << 62)); }
+// A wait within the CTA (nothing here waits for another).  False: it has run out, or another one has.  From then on a producer asks for no
+// further copy and arrives nowhere (a barrier that still counts a copy's bytes takes no arrival of the next turn), a consumer
+// takes and gives back no further tile, both walk their run to its end (so that barriers, tickets and the list of parts are as always), and the
+// results are no numbers.  What a producer has asked for lands before it leaves.
+__device__ __forceinline__ bool att_wait(uint32_t bar, uint32_t parity, uint32_t stop, Ctrl* ctrl) {
+    if (bar_test(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        long long cycles, dead;
+        asm volatile("ld.shared.v2.s64 {%0,%1}, [%2];" : "=l"(cycles), "=l"(dead) : "r"(stop) : "memory");
+        if (cycles < kAttShortWait ? bar_test(bar, parity) : bar_try(bar, parity)) return true;
+        if (dead) return false;
+        if (clock64() - t0 > cycles) {
+            asm volatile("st.shared.s64 [%0], %1;" ::"r"(stop + 8), "l"(1ll) : "memory");
             atomicOr(&ctrl->flags, (uint32_t)VT_FLAG_TIMEOUT);
-            return;
+            return false;
         }
     }
 }
@@ -547,7 +566,7 @@ struct AttProducer {
     using C = AttCfg<D, F8, WR>;
     const KvAttendArgs& a;
     const CUtensorMap *k_map, *v_map;
-    uint32_t ring, notes, full, empty, dead;                     // of this producer, in shared memory
+    uint32_t ring, notes, full, empty, stop;                     // of this producer, in shared memory
     int16_t* parents;
     const int* lens;
     AttWalk walk;
@@ -811,25 +830,29 @@ struct AttProducer {
         constexpr bool kLate = F8 && C::kPer >= 2 * kAttTurns;
         AttTokens now, next;                                     // page ids are asked for a round, exponents a round's copies ahead
         look_up(now);
-        while (now.have) {
+        for (bool stopped = false; now.have; now = next) {
             resolve(now);
             look_up(next);
-            int at = place;
+            if (stopped) continue;                               // (the walk has meetings of the four producers)
+            int at = place, asked = 0;
             uint32_t p = parity;
             // (a look at a barrier takes 200 cycles: at both places' at once)
-            bool given[kAttTurns];
+            bool given = C::kPer >= kAttTurns;
 #pragma unroll
-            for (int t = 0; t < kAttTurns; ++t) given[t] = bar_try(empty + 8 * ((place + t) % C::kPer), place + t >= C::kPer ? parity ^ 1 : parity);
+            for (int t = 0; t < kAttTurns; ++t) given &= bar_try(empty + 8 * ((place + t) % C::kPer), place + t >= C::kPer ? parity ^ 1 : parity);
+            given = __all_sync(0xffffffffu, given);
 #pragma unroll
             for (int t = 0; t < kAttTurns; ++t) {
-                if (!given[t] || C::kPer < kAttTurns) att_wait(empty + 8 * at, p, dead, a.ctrl);
+                if (!given) stopped = stopped || !__all_sync(0xffffffffu, att_wait(empty + 8 * at, p, stop, a.ctrl));
+                if (stopped) continue;
                 if (kAttTile * (kAttFeeds * t + feed) < now.n) copy(now, t, at);
                 if (!kLate) finish(now, t);
+                ++asked;
                 if (++at == C::kPer) at = 0, p ^= 1;
             }
 #pragma unroll
-            for (int t = 0; t < (kLate ? kAttTurns : 0); ++t) finish(now, t);
-            now = next;
+            for (int t = 0; t < (kLate ? kAttTurns : 0); ++t)
+                if (t < asked) finish(now, t);
         }
         // No copy is in flight when the CTA ends, also when a wait has run out: the last use of every place in the ring lands.
         for (int k = max(0, filled - C::kPer); k < filled; ++k) {
@@ -955,7 +978,8 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     __shared__ float s_qscale[C::kQRegs ? 1 : 16 * WR];          // powers that the queries' rows were scaled by, undone in the scores
     __shared__ long long s_sum[kAttWarps + kAttFeeds];
     __shared__ long long s_at, s_u[2];
-    __shared__ int s_seq, s_dead;
+    __shared__ int s_seq;
+    __shared__ AttStop s_stop;
     __shared__ AttWalk s_walk[kAttWarps];
     __shared__ AttSegment s_segment[kAttWarps];
     __shared__ long long s_first[kAttWarps];
@@ -970,7 +994,11 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         mbar_init(s_full + tid, 33);                             // the producer's lanes, by their copies, and its word that the rest is there
         mbar_init(s_empty + tid, WR);
     }
-    if (tid == 0) s_dead = 0, s_join[0].x = s_join[1].x = -1;
+    if (tid == 0) s_stop.cycles = bound_cycles(kAttWaitNs), s_stop.dead = 0, s_join[0].x = s_join[1].x = -1;
+    // the caller's bound, 0 = the default: written with the host waiting for it, so it is final before any later launch (it arrives while the work
+    // is dealt out)
+    unsigned long long bound = 0;
+    if (tid == kAttThreads - 1) bound = *reinterpret_cast<volatile unsigned long long*>(&a.ctrl->wait_ns);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     griddep_launch_dependents();
     __syncthreads();
@@ -1066,6 +1094,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         __syncthreads();
         walk.u = s_u[0], walk.u1 = s_u[1], walk.seq = s_seq, walk.off = s_at;
     }
+    if (bound) s_stop.cycles = bound_cycles(bound);
     if (walk.u >= walk.u1) {
         if (tid == 0 && !HALF) a.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
         return;
@@ -1075,7 +1104,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAttProducerRegs));
         const int feed = warp - kAttWarps;
         AttProducer<D, F8, WR> p{a, &k_map, &v_map, smem_u32(ring) + feed * C::kPer * C::kSlot, smem_u32(notes) + feed * C::kPer * C::kNote,
-                                 smem_u32(s_full + feed * C::kPer), smem_u32(s_empty + feed * C::kPer), smem_u32(&s_dead), parents, lens, walk, {},
+                                 smem_u32(s_full + feed * C::kPer), smem_u32(s_empty + feed * C::kPer), smem_u32(&s_stop), parents, lens, walk, {},
                                  groups, lane, feed, 0, -1, -1, -1, -1, -1};
         p.run();
         return;
@@ -1094,6 +1123,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
     att_next(a, lens, groups, walk, g);
     s_segment[warp] = g, s_walk[warp] = walk;
     q.fetch(a, g, warp, lane);
+    bool lost = false;                                           // one of the warp's waits has run out
     for (bool go_on = true; go_on;) {
         float scale[2];
         q.settle(a.scale_log2, scale, qs, s_qscale, warp, lane);
@@ -1101,9 +1131,10 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
 
         AttAcc<D> acc;
         acc.clear();
-        for (bool more = true; more;) {
+        for (bool more = !lost; more;) {
             const int slot = feed * C::kPer + place;
-            att_wait(smem_u32(s_full) + 8 * slot, parity, smem_u32(&s_dead), a.ctrl);
+            lost = !__all_sync(0xffffffffu, att_wait(smem_u32(s_full) + 8 * slot, parity, smem_u32(&s_stop), a.ctrl));
+            if (lost) break;
             const uint8_t* tile = ring + slot * C::kSlot;
             const uint8_t* note = notes + slot * C::kNote;
             const uint32_t header = ld_shared(smem_u32(note) + C::kHeader);
@@ -1122,7 +1153,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
                 place += C::kShare;
                 if (place >= C::kPer) place -= C::kPer, parity ^= 1;
             }
-            more = !(header & kAttEnd) && !ld_shared(smem_u32(&s_dead));
+            more = !(header & kAttEnd);
         }
 
         g = s_segment[warp];
@@ -1186,7 +1217,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         const int last_cta = whole ? 0 : (int)quotient((start + g.units - kAttSnap) * ctas - 1, total);
         if (!HALF && !whole && g.tile0 == 0) meta = make_int4(last_cta, g.seq, g.head, g.group);
         if (team != 0) continue;
-        const bool broken = ld_shared(smem_u32(&s_dead)) != 0;
+        const bool broken = ld_shared(smem_u32(&s_stop.dead)) != 0;
         float* part = a.part + (2 * (int64_t)blockIdx.x + (g.tile0 == 0 ? 1 : 0)) * a.part_rows * kv_part_floats(D);
 #pragma unroll
         for (int r = 0; r < (HALF ? 1 : 2); ++r) {
