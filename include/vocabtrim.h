@@ -427,7 +427,9 @@ vt_status vt_kv_attend(const uint16_t *q, int64_t q_ld, int32_t Q, int32_t Hq, c
  * nodes[s][path[s][i]] where `nodes` is given (vt_tree_rerank's out_nodes: the draft's positions as nodes of the pool), moves to
  * place lens[s] + i.  path, nodes [S,N]; a node smaller than i is out of range (paths rise).
  * new_lens [S] or NULL receives lens[s] + n_accept[s]; it may be `lens`.  A bit copy; every layer's cache is moved by
- * a call of its own, with the old lens.  lens or n_accept out of range: nothing moves.  `ws` as above.
+ * a call of its own, with the old lens.  lens or n_accept out of range (the page table holds fewer than their sum among it): nothing
+ * moves, new_lens is lens.  A single row that is left out (a node or a page out of range) still counts in new_lens: its place holds what lay
+ * there, and only VT_FLAG_BAD_PAGE tells, so pass `ws` where that can happen.
  */
 vt_status vt_kv_commit(const vt_kv_cache *cache, const int32_t *lens, const int32_t *path, const int32_t *n_accept,
                        const int32_t *nodes, int32_t N, int32_t *new_lens, void *ws, void *stream);

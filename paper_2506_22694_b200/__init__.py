@@ -475,7 +475,8 @@ def vt_kv_commit(cache, pages: torch.Tensor, lens: torch.Tensor, path: torch.Ten
                  nodes: torch.Tensor | None = None, out: torch.Tensor | None = None, ws: Workspace | None = None) -> torch.Tensor:
     """Accepted nodes become committed tokens (Algorithm 2's accept loop): the cached row of path[s][i], i < n_accept[s], moves to place
     lens[s] + i.  path and n_accept as vt_verify_greedy returns them; nodes int32 [S,N]: the draft's nodes in the pool (vt_tree_rerank's
-    first output) where the cache was written by pool node.  Returns the new lengths [S]; out may be lens."""
+    first output) where the cache was written by pool node.  Returns the new lengths [S]; out may be lens.  Rows that are out of range
+    are counted all the same and flagged in `ws`; a path that the page table cannot hold is not moved and not counted."""
     _lib or lib()
     r = _bind.kv_commit(cache, pages, lens, path, n_accept, nodes, out, ws)
     if r.__class__ is int:

@@ -429,7 +429,7 @@ k_kv_commit(const __grid_constant__ KvCommitArgs a) {
     const bool e4m3 = a.c.k_exp != nullptr;
     int32_t len = ld_cg_s32(a.lens + s), n = ld_cg_s32(a.n_accept + s);
     const int64_t room = (int64_t)a.c.max_pages * a.c.page;
-    const bool bad = len < 0 || len > room || n < 0 || n > a.N;
+    const bool bad = len < 0 || len > room || n < 0 || n > a.N || (int64_t)len + n > room;
     if (bad) n = 0;
     __syncthreads();                                             // (new_lens may be lens: every thread has read it)
     if (threadIdx.x == 0) {

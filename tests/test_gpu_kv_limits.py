@@ -28,3 +28,27 @@ def test_attention_over_the_longest_sequence():
     off = n / (148 * 8 * 32) * 4 * 2.0 ** -24 + 2.0 ** -18
     assert float((out.float() / one.float() - 1).abs().max()) <= 2 * off + 2.0 ** -7
     assert float((lse - one_lse - math.log(times)).abs().max()) <= off + 2.0 ** -18
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_path_that_the_page_table_cannot_hold_is_not_committed(e4m3):
+    """Not in part, and it does not count: lengths never pass what the table holds."""
+    host = ku.Host(4, 40, 2, 64, 10, e4m3, seed=2)
+    lens, n_accept = torch.tensor([38, 38, 40, 37], dtype=I32).cuda(), torch.tensor([2, 3, 1, 3], dtype=I32).cuda()
+    path = torch.tensor([[0, 1, 2, 3], [1, 2, 3, -1], [0, -1, -1, -1], [0, 1, 2, -1]], dtype=I32).cuda()
+    ws = vt.Workspace(vt.VT_CTRL_BYTES)
+    assert host.pages.shape[1] * host.page == 40
+    assert vt.vt_kv_commit(host.device(), host.pages_dev, lens, path, n_accept, ws=ws).tolist() == [40, 38, 40, 40]
+    assert host.same() and ws.read_status()[:2] == (2, vt.VT_FLAG_BAD_PAGE)
+    assert vt.vt_kv_commit(host.dev, host.pages_dev, lens, path, n_accept, out=lens, ws=ws) is lens and lens.tolist() == [40, 38, 40, 40]
+
+
+def test_a_path_at_the_end_of_the_longest_sequence():
+    page, times = 32 * 2731, 24573
+    k = ku.bf16((1, 1, page, 64), 1).cuda()
+    v, pages, room = k.clone(), torch.zeros((1, times), dtype=I32, device="cuda"), page * times
+    path, ws = torch.arange(100, dtype=I32, device="cuda")[None], vt.Workspace(vt.VT_CTRL_BYTES)
+    for n, taken in ((31, 31), (32, 0), (100, 0)):
+        n_accept, lens = torch.tensor([n], dtype=I32).cuda(), torch.tensor([room - 31], dtype=I32).cuda()
+        assert vt.vt_kv_commit((k, v), pages, lens, path, n_accept, ws=ws).tolist() == [room - 31 + taken]
+        assert ws.read_status()[1] == (0 if taken else vt.VT_FLAG_BAD_PAGE)
