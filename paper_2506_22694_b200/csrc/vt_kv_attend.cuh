@@ -1339,6 +1339,7 @@ cudaError_t attend_go(const KvAttendArgs& a, int& ctas, cudaStream_t s) {
         const bool same = kept.set && kept.c.page == a.c.page && kept.c.heads == a.c.heads && kept.c.n_pages == a.c.n_pages &&
                           kept.c.stride_token == a.c.stride_token && kept.c.stride_head == a.c.stride_head && kept.c.stride_page == a.c.stride_page;
         if (!same) {
+            kept.set = false;                                    // (a shape that is refused leaves no map behind)
             if (!kv_map(&kept.map, a.c, a.c.k, F8, C::kBox)) return cudaErrorInvalidValue;
             kept.c = a.c, kept.set = true;
         }

@@ -1,4 +1,5 @@
 """The cache's calls at the end of the range of places that a page table may span."""
+import ctypes
 import math
 
 import pytest
@@ -6,6 +7,7 @@ import torch
 
 import kv_util as ku
 import paper_2506_22694_b200 as vt
+from test_kv_refusals import KV
 
 pytestmark = pytest.mark.gpu
 I32 = torch.int32
@@ -52,3 +54,19 @@ def test_a_path_at_the_end_of_the_longest_sequence():
         n_accept, lens = torch.tensor([n], dtype=I32).cuda(), torch.tensor([room - 31], dtype=I32).cuda()
         assert vt.vt_kv_commit((k, v), pages, lens, path, n_accept, ws=ws).tolist() == [room - 31 + taken]
         assert ws.read_status()[1] == (0 if taken else vt.VT_FLAG_BAD_PAGE)
+
+
+def test_a_cache_that_no_tensor_map_describes_leaves_the_next_call_alone():
+    """A stride of 2^40 bytes (of one page, never stepped over) is refused on the host, between two calls of another shape."""
+    host = ku.Host(2, 100, 2, 64, 16, False, seed=3)
+    dev, lens, q = host.device(), torch.tensor([100, 61], dtype=I32).cuda(), ku.bf16((2, 4, 64), 5).cuda()
+    ws = ku.attend_ws(2, 1, 4, 2, 64)
+    good = vt.vt_kv_attend(q, dev, host.pages_dev, lens, ws=ws)
+    wide = KV(k=dev[0].data_ptr(), v=dev[1].data_ptr(), k_exp=None, v_exp=None, format=0, n_pages=1, heads=2, page=16, d=64, stride_page=2 ** 39,
+              stride_head=16 * 64, stride_token=64, pages=host.pages_dev.data_ptr(), S=2, max_pages=host.pages.shape[1], pages_ld=host.pages.shape[1])
+    out = torch.empty_like(good[0])
+    stream = torch.cuda.current_stream().cuda_stream
+    assert vt.lib().vt_kv_attend(q.data_ptr(), 256, 1, 4, ctypes.byref(wide), lens.data_ptr(), None, None, 0, 0, 0.125, out.data_ptr(), None, ws.ptr, ws.nbytes,
+                                 stream) != vt.VT_OK
+    got = vt.vt_kv_attend(q, dev, host.pages_dev, lens, ws=ws)
+    assert torch.equal(got[0], good[0]) and torch.equal(got[1], good[1]) and ws.read_status() == (0, 0, 0)
