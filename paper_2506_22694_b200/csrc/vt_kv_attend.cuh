@@ -529,7 +529,7 @@ __device__ __forceinline__ int att_len(const KvAttendArgs& a, int s) {
     return (int)min((int64_t)max(ld_cg_s32(a.lens + s), 0), (int64_t)a.c.max_pages * a.c.page);
 }
 __device__ __forceinline__ int att_units(const KvAttendArgs& a, int len) {
-    return (int)(((uint32_t)len + kAttUnit - 1) / kAttUnit) + kAttPairUnits + (a.node ? kAttTreeUnits : 0);
+    return len / kAttUnit + (len % kAttUnit != 0) + kAttPairUnits + (a.node ? kAttTreeUnits : 0);
 }
 __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens, int groups, AttWalk& w, AttSegment& g) {
     if (w.u >= w.u1) return false;
@@ -1172,7 +1172,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
 
         // the teams' parts meet, the upper half's with the lower half's: a lane hands its share to the lane with the same rows and dims
         // (of a short segment's teams only the first have had tokens)
-        const int active = (int)min(((uint32_t)max(g.token_end - g.token, g.tree ? a.N : 0) + C::kTile - 1) / C::kTile, (uint32_t)C::kTeams);
+        const int active = (min(max(g.token_end - g.token, g.tree ? a.N : 0), C::kTeams * C::kTile) + C::kTile - 1) / C::kTile;
         if (active > 1 || !C::kQRegs) consumers_barrier();       // (the meeting place is free, and so are the queries' rows)
         bool first_step = true;
 #pragma unroll
