@@ -53,7 +53,6 @@ constexpr int kCh = 16;                   // accumulator columns per epilogue st
 constexpr int kParts = 2;                  // epilogue warps per TMEM lane quadrant
 constexpr int kTmemCols = 512;            // 2 accumulator stages x kMaxBN columns
 constexpr int kMaxTopk = 16;              // the list's values live in registers
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 constexpr size_t kSmemBudget = 225 * 1024;   // ring and candidate entries at most (227 KB per CTA less alignment slack and statics)
 // What of it a pair leaves to L1 where the uniforms come one by one (K no multiple of four, or an unaligned pointer).  Sixteen loads then
 // share the 256 lines of the eight epilogue warps, 32 KB; beside more than 196 KB of shared memory L1 has 28 KB, and 60 beside this.

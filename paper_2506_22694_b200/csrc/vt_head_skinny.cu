@@ -55,7 +55,6 @@ constexpr int kMaxB = 64;
 // started 2-3 us after all others (one row, L2: 5000 x 3072 12.9 -> 11.7 us, 5000
 // x 4096 14.6 -> 13.2).
 constexpr size_t kSmemLimit = 228 * 1024 - (1024 + 512) - (kMergeStageWords * 4 + 1024 + 128);
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // default bound of a device-side wait (Ctrl::wait_ns overrides)
 
 // Phase stamps (-DVT_STAMPS builds only): one thread per role writes %globaltimer at fixed points into
 // a region behind the records; bench.py --case stamps reads them back.  Slots: 0 entry, 1 ring fill
@@ -89,23 +88,6 @@ struct Geo {
 };
 
 // ---- bounded waits ---------------------------------------------------------------------------------
-// non-blocking probe of a phase (try_wait may suspend the thread for a system-chosen time before it answers)
-__device__ __forceinline__ bool mbar_test(uint64_t* b, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-        : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
-    return ok != 0;
-}
-// The bound of a wait is kept with the SM's cycle counter (reading the nanosecond timer costs far more
-// than a probe): two cycles per nanosecond, i.e. at least the time asked for at any SM clock up to
-// 2 GHz.  It lives in shared memory and is looked at only once a wait has to spin.  Bounds under a
-// millisecond spin on non-blocking probes only: try_wait may park the thread for a system-chosen time before
-// it answers, which is what a long wait wants and a short bound cannot afford.
-__device__ __forceinline__ long long bound_cycles(unsigned long long ns) {
-    return (long long)(ns < (1ull << 61) ? 2 * ns : (1ull << 62));
-}
-constexpr long long kShortBoundCycles = 2000000;      // 1 ms
 // Bounded wait of one thread; false when the CTA is aborting or the bound expired (which starts an abort).  A role that
 // waits before the launch dependency is released passes `released`: earlier work on the stream does not count, the clock
 // starts when that flag is up (until then the bound is a thousand times the default).

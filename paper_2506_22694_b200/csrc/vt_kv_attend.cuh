@@ -59,7 +59,6 @@ constexpr int kAttLens = 1024;                                   // sequences wh
 constexpr int kAttTile = 32;                                      // tokens of a tile: one of each lane of the producer that fills it
 constexpr int kAttTurns = 2;                                     // tiles of a producer in a round
 constexpr int kAttRound = kAttTile * kAttFeeds * kAttTurns;      // tokens that the producers look up at a time
-constexpr unsigned long long kAttWaitNs = 2000000000ull;         // bound of a wait where the workspace has none, and of copies in flight at the end
 
 template <int D, bool F8, int WR>
 struct AttCfg {
@@ -102,12 +101,6 @@ struct AttCfg {
 // bf16: whether there is no such token.
 enum { kAttEnd = 1, kAttEmpty = 2, kAttTree = 4, kAttShort = 8 };            // a tile's header (short: some tokens are missing)
 
-// One lane of a converged warp: the compiler then knows that one thread is active.
-__device__ __forceinline__ bool elect_lane() {
-    uint32_t r;
-    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
-    return r != 0;
-}
 // 16 bytes, or zeros where `have` is false (then the source is not read)
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool have) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
@@ -138,11 +131,6 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, ui
 __device__ __forceinline__ float exp2_fast(float x) {            // ex2.approx: 2 ulp; weights below 2^-126 are zero
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float exp2_whole(float x) {           // with results below 2^-126
-    float y;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -195,19 +183,6 @@ __device__ __forceinline__ void consumers_barrier() { asm volatile("bar.sync 15,
 
 __device__ __forceinline__ void feeds_barrier() { asm volatile("bar.sync 14, %0;" ::"n"(32 * kAttFeeds) : "memory"); }
 
-// The mbarriers by their addresses in shared memory: 32 bits, of which the warps here keep many.
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// (without parking the thread)
-__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {       // without arriving
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
@@ -221,14 +196,11 @@ __device__ __forceinline__ uint32_t ld_shared(uint32_t at) {
     return x;
 }
 
-// What bounds a CTA's waits, in shared memory.  The bound is kept with the SM's cycle counter, two cycles a nanosecond: at least the time asked
-// for at any clock up to 2 GHz.  Bounds under a millisecond spin on probes that do not park the thread.
+// What bounds a CTA's waits, in shared memory.
 struct __align__(16) AttStop {
-    long long cycles;
-    long long dead;               // a wait has run out
+    long long cycles;             // the bound of each
+    long long dead;               // one has run out
 };
-constexpr long long kAttShortWait = 2000000;
-__device__ __forceinline__ long long bound_cycles(unsigned long long ns) { return (long long)(ns < (1ull << 61) ? 2 * ns : (1ull << 62)); }
 // A wait within the CTA (nothing here waits for another).  False: it has run out, or another one has.  From then on a producer asks for no
 // further copy and arrives nowhere (a barrier that still counts a copy's bytes takes no arrival of the next turn), a consumer
 // takes and gives back no further tile, both walk their run to its end (so that barriers, tickets and the list of parts are as always), and the
@@ -239,7 +211,7 @@ __device__ __forceinline__ bool att_wait(uint32_t bar, uint32_t parity, uint32_t
     for (;;) {
         long long cycles, dead;
         asm volatile("ld.shared.v2.s64 {%0,%1}, [%2];" : "=l"(cycles), "=l"(dead) : "r"(stop) : "memory");
-        if (cycles < kAttShortWait ? bar_test(bar, parity) : bar_try(bar, parity)) return true;
+        if (cycles < kShortBoundCycles ? bar_test(bar, parity) : bar_try(bar, parity)) return true;
         if (dead) return false;
         if (clock64() - t0 > cycles) {
             asm volatile("st.shared.s64 [%0], %1;" ::"r"(stop + 8), "l"(1ll) : "memory");
@@ -550,7 +522,6 @@ __device__ __forceinline__ bool att_next(const KvAttendArgs& a, const int* lens,
 
 enum { kChain, kLevels, kNodes };                                // how a producer finds a tree's nodes
 constexpr int kAttDeep = 64;                                     // depths that are walked in step
-constexpr int kAttHeld = 1;                                      // parents that a producer's lane asks for at a time
 
 // A producer's lane: its tokens of a round, one of each tile.
 struct AttTokens {
@@ -577,7 +548,7 @@ struct AttProducer {
     int f0, f1;                   // where those have got to
     int way = 0, depth = 0, most = 0;                            // how nodes are found; of row lane's node (-1: none), and of all rows'
     int level = 0;                // where the search is
-    int held[kAttHeld];           // parents on their way
+    int held;                     // a parent on its way
     bool fresh = false, begun = false;                           // the tree's loads are in flight; the segment's tree has been begun
     int place = 0, filled = 0;    // of the next tile, in the ring; tiles so far
     uint32_t parity = 1;          // (an empty ring's places count as given back)
@@ -679,11 +650,8 @@ struct AttProducer {
         n0 = lane < a.Q ? ld_cg_s32(a.node + (int64_t)g.seq * a.Q + lane) : -1;
         n1 = lane + 32 < a.Q ? ld_cg_s32(a.node + (int64_t)g.seq * a.Q + lane + 32) : -1;
         if (!a.parent) return;
-#pragma unroll
-        for (int k = 0; k < kAttHeld; ++k) {
-            const int i = 32 * (kAttFeeds * k + feed) + lane;
-            held[k] = i < a.N ? ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i) : -1;
-        }
+        const int i = 32 * feed + lane;
+        held = i < a.N ? ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i) : -1;
     }
     // ... and what it takes to find the nodes that some row sees, each once, with the rows that see it: of a chain all up to the largest; in a
     // tree the rows (32 at the most) walk to the root in step, by depth; where there are more rows or a node lies deep, they are merged node by
@@ -702,9 +670,8 @@ struct AttProducer {
                 auto keep = [&](int i, int p) {
                     if (i < N) parents[i] = (int16_t)(p >= 0 && p < i ? p : -1);           // (a parent that does not lie in front ends the walk)
                 };
-#pragma unroll
-                for (int k = 0; k < kAttHeld; ++k) keep(32 * (kAttFeeds * k + feed) + lane, held[k]);
-                for (int i = 32 * (kAttFeeds * kAttHeld + feed) + lane; i < N; i += 32 * kAttFeeds)
+                keep(32 * feed + lane, held);
+                for (int i = 32 * (kAttFeeds + feed) + lane; i < N; i += 32 * kAttFeeds)
                     keep(i, ld_cg_s32(a.parent + (int64_t)g.seq * a.parent_ld + i));
                 feeds_barrier();
                 way = a.Q > 32 ? kNodes : kLevels;
@@ -746,7 +713,7 @@ struct AttProducer {
             const int id0 = __shfl_sync(0xffffffffu, id, 0), in0 = __shfl_sync(0xffffffffu, in, 0);
             if (id0 >= 0) {
                 boxed = 0xffffffffu;
-                if (elect_lane()) {
+                if (elect_one()) {
                     if (dirty >> at & 1) fence_async();          // (what threads have stored there comes first)
                     bar_expect(bar, 2 * 32 * C::kRow);
 #pragma unroll
@@ -765,7 +732,7 @@ struct AttProducer {
             const int id0 = __shfl_sync(0xffffffffu, id, 0), in0 = __shfl_sync(0xffffffffu, in, 0);
             const int id1 = __shfl_sync(0xffffffffu, id, 16), in1 = __shfl_sync(0xffffffffu, in, 16);
             boxed = (id0 >= 0 ? 0xffffu : 0u) | (id1 >= 0 && rest >= 32 ? 0xffff0000u : 0u);
-            if (boxed && elect_lane()) {
+            if (boxed && elect_one()) {
                 if (dirty >> at & 1) fence_async();
                 bar_expect(bar, __popc(boxed) * 2 * C::kRow);
 #pragma unroll
@@ -857,7 +824,7 @@ struct AttProducer {
         // No copy is in flight when the CTA ends, also when a wait has run out: the last use of every place in the ring lands.
         for (int k = max(0, filled - C::kPer); k < filled; ++k) {
             const unsigned long long t0 = global_ns();
-            while (!bar_try(full + 8 * (k % C::kPer), k / C::kPer & 1) && global_ns() - t0 < kAttWaitNs) {}
+            while (!bar_try(full + 8 * (k % C::kPer), k / C::kPer & 1) && global_ns() - t0 < kWaitLimitNs) {}
         }
     }
     __device__ __forceinline__ void finish(const AttTokens& r, int t) {
@@ -994,7 +961,7 @@ k_kv_attend(const __grid_constant__ KvAttendArgs a, const __grid_constant__ CUte
         mbar_init(s_full + tid, 33);                             // the producer's lanes, by their copies, and its word that the rest is there
         mbar_init(s_empty + tid, WR);
     }
-    if (tid == 0) s_stop.cycles = bound_cycles(kAttWaitNs), s_stop.dead = 0, s_join[0].x = s_join[1].x = -1;
+    if (tid == 0) s_stop.cycles = bound_cycles(kWaitLimitNs), s_stop.dead = 0, s_join[0].x = s_join[1].x = -1;
     // the caller's bound, 0 = the default: written with the host waiting for it, so it is final before any later launch (it arrives while the work
     // is dealt out)
     unsigned long long bound = 0;

@@ -1,4 +1,4 @@
-// Tensor-core plumbing shared by the two head kernels: mbarrier and TMA wrappers, tcgen05 operand and
+// Tensor-core plumbing shared by the two head kernels: TMA wrappers, tcgen05 operand and
 // instruction descriptors, and the host-side encoding of the tensor maps.
 #pragma once
 #include "vt_maps.cuh"
@@ -9,15 +9,6 @@ namespace {
 
 constexpr int kBK = 64;                   // columns of d per tensor copy: 128 bytes, one swizzle row
 
-// One lane of a converged warp.  The single-thread roles (copy producer, MMA issuer) are entered through this and
-// not through `lane == 0`: behind elect.sync the compiler knows that one thread is active and hands tcgen05 and
-// copy instructions their operands in uniform registers; behind a comparison it guards every one of them against
-// a divergent warp (measured: 70-105 cycles to issue an MMA of M = 128, N = 16 instead of the 40 it takes).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
-    return r != 0;
-}
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
