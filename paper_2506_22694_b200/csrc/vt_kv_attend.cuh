@@ -804,13 +804,13 @@ struct AttProducer {
             int at = place, asked = 0;
             uint32_t p = parity;
             // (a look at a barrier takes 200 cycles: at both places' at once)
-            bool given = C::kPer >= kAttTurns;
+            bool given[kAttTurns];
 #pragma unroll
-            for (int t = 0; t < kAttTurns; ++t) given &= bar_try(empty + 8 * ((place + t) % C::kPer), place + t >= C::kPer ? parity ^ 1 : parity);
-            given = __all_sync(0xffffffffu, given);
+            for (int t = 0; t < kAttTurns; ++t) given[t] = bar_try(empty + 8 * ((place + t) % C::kPer), place + t >= C::kPer ? parity ^ 1 : parity);
 #pragma unroll
             for (int t = 0; t < kAttTurns; ++t) {
-                if (!given) stopped = stopped || !__all_sync(0xffffffffu, att_wait(empty + 8 * at, p, stop, a.ctrl));
+                const bool here = (C::kPer >= kAttTurns && given[t]) || (!stopped && att_wait(empty + 8 * at, p, stop, a.ctrl));
+                stopped = !__all_sync(0xffffffffu, here && !stopped);
                 if (stopped) continue;
                 if (kAttTile * (kAttFeeds * t + feed) < now.n) copy(now, t, at);
                 if (!kLate) finish(now, t);
