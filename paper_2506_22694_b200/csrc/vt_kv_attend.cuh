@@ -138,7 +138,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Four e4m3 bytes as two pairs of f16 (exact).  In a tree's tile (FINITE) by their bits, moved to f16's places, which is the value times
+// Four e4m3 bytes as two pairs of f16 (exact).  A tree's values (FINITE) by their bits, moved to f16's places, which is the value times
 // 2^-8, and one exact multiplication: a NaN byte then is a number, and a weight of zero keeps it out of the rows that do not see it.
 template <bool FINITE>
 __device__ __forceinline__ void e4m3_pairs(uint32_t x, uint32_t& lo, uint32_t& hi) {
@@ -277,7 +277,7 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {                    // i: (token half, dim half)
                     uint32_t lo, hi;
-                    e4m3_pairs<LIST>(b[i], lo, hi);
+                    e4m3_pairs<false>(b[i], lo, hi);
                     mma<true>(s[2 * g + (i >> 1)], qa[i & 1], lo, hi);
                 }
             }
@@ -310,16 +310,6 @@ __device__ __forceinline__ void att_tile(AttAcc<D>& acc, const uint32_t (*qf)[4]
                 const uint32_t x = *reinterpret_cast<const uint32_t*>(note + C::kToken * (8 * i + 2 * j + u));
                 if (F8 ? !x : x) s[i][u] = s[i][2 + u] = -INFINITY;
             }
-    }
-    if (F8 && LIST) {                                            // (a NaN went through the product as a number: it is one for the rows that see it)
-        const uint32_t bad = nan_tokens<C>(slot, lane);
-        if (bad) {
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    if (bad >> (8 * i + 2 * j + u) & 1) s[i][u] = s[i][2 + u] = NAN;
-        }
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
