@@ -78,8 +78,8 @@ struct KvAttendArgs {
 __host__ __device__ constexpr int kv_part_floats(int d) { return d + 3; }
 int kv_attend_warp_rows(int rows, int d);        // warps side by side over a key head's rows (1, 2 or 4 of 16 rows each)
 // Whether the attention kernel joins its parts itself: up to eight rows.  The CTA whose part arrives last reads them all, 40 KB for four rows and 19
-// parts; a kernel of its own, which deals more rows out to all CTAs, costs 1 to 2 us more for one token (256 tokens 11.7 us for 9.9, 701 13.6
-// for 12.7) and less for a batch whose CTAs all end at once (64 sequences 169 us for 172).
+// parts; a kernel of its own, which deals more rows out to all CTAs, costs 1 to 2 us more for one token (256 tokens 10.1 us for 8.4, 701 12.6
+// for 11.3, 4000 14.4 for 12.6) and 1 to 5 for a batch (64 sequences in bf16 178 us for 177, in e4m3 120 for 115).
 inline bool kv_attend_joins(int rows, int d) { return rows <= 8 && d <= 128; }
 size_t kv_attend_scratch_bytes(int rows, int d);
 cudaError_t launch_kv_attend_bf16(const KvAttendArgs& a, int& ctas, cudaStream_t s);

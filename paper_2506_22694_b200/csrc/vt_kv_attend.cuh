@@ -16,8 +16,9 @@
 // delivers it), and it keeps scores and weights in registers, where tcgen05 would send both through TMEM for tiles of 128 rows that
 // are seven eighths empty.
 //
-// Measured (heads of 128, 8 key heads): 64 sequences of up to 8000 tokens, bf16, 172 us, 92% of what copying HBM reaches; e4m3 104 us, 77%: there the
-// producers' instructions bound it (a tile has half the bytes and the exponents on top).  One sequence of 4000 tokens: 14 us, of which 7 are
+// Measured (heads of 128, 8 key heads): 64 sequences of up to 8000 tokens, bf16, 170 us, 93% of what copying HBM reaches; e4m3 114 us, 70%: there a
+// tile's instructions on twelve warps bound it (half the bytes, but conversions, exponents and a second exponential on top).  32 rows a head of 64 in
+// e4m3, 24%: 44% of the issue slots are used, a third of the stalls wait for the instruction before.  One sequence of 4000 tokens: 12.4 us, of which 6.7 are
 // what a call of 64 tokens takes: 1.7 before it starts, lengths and shares 1, page ids and first copies 1.7, a tile 0.8, meeting
 // and results 1.7.  The rest: another tile a team, the fence and the ticket of a part 0.9, the join 1.6.
 //
@@ -48,11 +49,12 @@ constexpr int kAttConsumerRegs = 200, kAttProducerRegs = 104;
 static_assert(kAttWarps * kAttConsumerRegs + kAttFeeds * kAttProducerRegs <= (kAttWarps + kAttFeeds) * 168, "what the block was launched with");
 constexpr int kAttUnit = 64;                                     // tokens
 // What a result counts for besides its tokens when the work is dealt out (the walk to it, its queries, the meeting), and a tree's tokens.
-// 64 ragged sequences of up to 8000 tokens, us with 2 / 4 / 8 / 12 for a result (parts still joined by a second launch): bf16 186 / 174 / 169 / 170,
-// e4m3 145 / 133 / 115 / 112.
+// Single calls, L2 flushed, us with 4 / 8 / 12 for a result: 64 ragged sequences of up to 8000 tokens, bf16 187 / 189 / 191, e4m3 136 / 121 / 120; 16 of up
+// to 3000, bf16, 39 / 41 / 43.  With 4 / 8 / 12 / 16 / 24 for a tree: one over 4001 tokens 31.8 / 29.7 / 29.7 / 29.7 / 29.7, eight over 1000
+// 31.8 / 31.8 / 31.9 / 31.8 / 34.7, 32 over 6000 in e4m3 72.7 / 74.8 / 74.8 / 74.9 / 78.8.
 constexpr int kAttPairUnits = 8, kAttTreeUnits = 12;
-// No result is split so near to its ends.  2 / 4 / 6 / 10: a tree over 4001 tokens 21.7 / 23.1 / 26.2 / 32.3 us, a token over 1024 12.7 / 14.4 /
-// 14.6 / 15.2, batches alike.
+// No result is split so near to its ends.  2 / 4 / 6: a tree over 4001 tokens 19.8 / 21.3 / 23.8 us, a token over 1024 10.8 / 12.5 / 13.1, over 4000
+// 12.6 / 13.1 / 14.5, batches alike.
 constexpr int kAttSnap = 2;
 constexpr float kAttLift = 11.0f;                                // e4m3: weights of values are 2^11 to 2^15 at the most, of f16's 65504
 constexpr int kAttLens = 1024;                                   // sequences whose lengths are kept in shared memory

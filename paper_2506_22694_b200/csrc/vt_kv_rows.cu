@@ -84,8 +84,8 @@ __device__ __forceinline__ F group_sum(F x) {
     return x;
 }
 
-// Two fp32 operations in one instruction: a prompt's rows are bound by the instructions that they take (4140 a token of 48 heads with
-// scalar operations and exact divisions: 60 us for 8.5k tokens).
+// Two fp32 operations in one instruction: a prompt's rows are not far from being bound by the instructions that they take (4140 a token of 48
+// heads with scalar operations and exact divisions: 60 us for 8.5k tokens, now 48).
 typedef unsigned long long f2;
 __device__ __forceinline__ f2 two(float lo, float hi) { return ((f2)__float_as_uint(hi) << 32) | __float_as_uint(lo); }
 __device__ __forceinline__ float lo_of(f2 x) { return __uint_as_float((uint32_t)x); }
@@ -210,9 +210,10 @@ __device__ __forceinline__ uint2 to_e4m3(const F* x, uint32_t& exp_byte) {
 
 // ---- write ------------------------------------------------------------------------------------------------------
 // A warp takes a share of one token's heads, 32 / LG heads at a time, queries first, then keys, then values: the token's sines are made
-// once for all of them.  For prompts bound by the memory and, close behind, by instructions (the head size is a constant for their sake);
-// latency-bound for a token: `shares` spreads a few tokens over more warps.  8.5k tokens of 48 heads of 128 in bf16 (209 MB) take 49 us, 66%
-// of what copying HBM reaches; the same loads and stores without the arithmetic took 42.  One token: 5 us.
+// once for all of them.  Latency-bound for a token: `shares` spreads a few tokens over more warps.  8.5k tokens of 48 heads of 128 in bf16 (209 MB)
+// take 48.5 us, 67% of what copying HBM reaches: the same loads and stores without the arithmetic took 42 (8 bytes a lane, a warp's stores in front
+// of its next loads, a third of the seats taken), and the instructions use some 45% of the issue slots.  Into e4m3, keys in 64 bits,
+// 90 us with the reading back behind it.  One token: 5 us.
 template <int D>
 struct Rows {
     static constexpr int kLanes = D <= 64 ? 8 : D <= 128 ? 16 : 32, kHeads = 32 / kLanes, kStep = kHeads * D;      // of a pass
