@@ -160,7 +160,7 @@ class Workspace:
         _check("vt_workspace_init", lib().vt_workspace_init(c_void_p(self.ptr), self.nbytes, _stream()))
 
     def set_wait_limit(self, nanoseconds: int) -> None:
-        """Bound of every device-side wait of the streaming head kernel (0 = the default of 2 s)."""
+        """Bound of every device-side wait of the streaming head kernel and of vt_kv_attend (0 = the default of 2 s)."""
         _check("vt_workspace_set_wait_limit",
                lib().vt_workspace_set_wait_limit(c_void_p(self.ptr), int(nanoseconds), _stream()))
 
